@@ -420,6 +420,99 @@ int cf_decode_append(const cf_geom* geom, int32_t n_requests, int32_t cache_rows
                      void* k_final, void* v_final, int64_t kv_layer_stride, const int32_t* rows, int32_t step,
                      const void* k_new, const void* v_new, int64_t new_layer_stride, int32_t* status, void* stream);
 
+/* ------------------------------------------------------------------- paged cache held in 4 bits
+ * Decoding over caches that grow and end at different times, a quarter of the size.  The rows of a request lie in pages of
+ * page_rows rows; `table` names a request's pages, in order.  Everything that changes is DEVICE memory owned by the caller, so
+ * lengths that are decided on the device (final_rows of cf_assemble_final_cache) need not visit the host:
+ *     cf_pages_init(pages)                                           once
+ *     cf_assemble_final_cache(..., out_rows, k_out, v_out, final_rows)
+ *     cf_pages_resize(pages, final_rows, 0, out_rows, slots)         pages for the final caches, a slot for every row
+ *     cf_kv4_write(pages, ..., n_requests * out_rows, slots, k_out, v_out, ..., kv4)
+ * and a step t = 0, 1, ... of the decoding loop is
+ *     cf_pages_resize(pages, final_rows, t + 1, 1, slots)            once per step: one more row for each request
+ *     cf_kv4_write(pages, ..., n_requests, slots, k_new, v_new, ..., kv4)          per layer, or for several at once
+ *     cf_kv4_attn(pages, ..., q, ..., kv4, ...)                                    per layer, or for several at once
+ *
+ * Format.  A row of a kv head is cut into groups of 32 dims.  A group has a bf16 scale s, its largest magnitude over 6 rounded
+ * to nearest even, and every number x is kept as s times the nearest to x / s of 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a sign (ties to
+ * the even code: 0, 1, 2, 4 before 0.5, 1.5, 3, 6; magnitudes above 6 to 6).  s < 2^-126 is stored as 0 and the group as zeros; a
+ * group with a number that is not finite reads as NaN.  4.5 bits per number.  A slot is page * page_rows + row.  A layer of
+ * the pool is [n_pages][n_kv_heads][page_rows / 16] blocks of 18 * head_dim bytes, each with 16 rows of one kv head (D = head_dim):
+ *     0     key codes    row r at r D/2: dims 32 j + 8 t + i (t < 4, i < 8) at t D/8 + 4 j + i / 2
+ *     8 D   value codes  row 8 h + 2 t + p at h 4 D + t D/8 + p D/16: dims 32 j + 4 u + i (u < 8, i < 4) at u D/2 + 2 j + i / 2
+ *     16 D  key scales   bf16 [16][D/32]
+ *     17 D  value scales bf16 [16][D/32]
+ * A code is 4 bits: the number's place in the list above, and 8 for the sign; a byte's low half holds the even dim. */
+typedef struct cf_pages {
+    int32_t n_requests;       /* 1 .. 2^20                                                            */
+    int32_t page_rows;        /* rows of a page, a multiple of 16                                     */
+    int32_t n_pages;          /* pages of the pool                                                    */
+    int32_t table_cols;       /* most pages of a request                                              */
+    int32_t* table;           /* device [n_requests][table_cols]                                      */
+    int32_t* rows;            /* device [n_requests] rows in use                                      */
+    int32_t* free_pages;      /* device [n_pages] a stack: the first *free_count entries are free     */
+    int32_t* free_count;      /* device [1]                                                           */
+    int32_t* status;          /* device [1] first CF_ERR_* raised on the device, 0 if none            */
+} cf_pages;
+
+/* No request has rows, every page is free (page 0 is taken first), table entries are -1, status 0. */
+int cf_pages_init(const cf_pages* pages, void* stream);
+
+/* Requests grow, shrink or end: request b is to have rows[b] + extra_rows rows (none where rows[b] is negative, whatever
+ * extra_rows is).  Pages that are no longer needed are pushed on the stack, last request and last column first, and their
+ * table entries become -1; then the growing requests take pages from its top, in order: a request gets all that it needs, or
+ * none where it and those before it need more than there are.  Growing and shrinking back leaves the stack as it was.
+ *   rows   device [n_requests]; may be pages->rows itself
+ *   slots  device [n_requests][max_new], or NULL with max_new = 0: the slots of request b's new rows, in order, then -1
+ * Raised in the status word: CF_ERR_RANGE for a request that asks for fewer than 0 rows, more than table_cols * page_rows, or
+ * more new ones than max_new (where slots are given); CF_ERR_WORKSPACE for one that the pool has no pages for.  Such a
+ * request keeps its rows and gets no slots; requests behind it that need no page are served. */
+int cf_pages_resize(const cf_pages* pages, const int32_t* rows, int32_t extra_rows, int32_t max_new, int64_t* slots,
+                    void* stream);
+
+/* Copies the status word back (synchronises `stream`); returns it as the error code. */
+int cf_pages_status(const cf_pages* pages, void* stream);
+
+/* Bytes of a layer of the pool for this geometry; 0 on invalid arguments. */
+size_t cf_kv4_layer_bytes(const cf_geom* geom, const cf_pages* pages);
+
+/* Rows of keys and values into their slots, in every layer.
+ *   slots   device [n_rows]: where row i goes; negative: nowhere.  A slot that appears twice is left with one row's numbers or
+ *           another's, which may differ from group to group
+ *   k, v    device, storage type of geom: layer l's row i at l * kv_layer_stride + i * row_stride elements,
+ *           [n_kv_heads][head_dim] each; strides are multiples of 16 bytes
+ *   kv4     the pool, layers kv4_layer_stride bytes apart (a multiple of 16)
+ * A slot beyond the pool raises CF_ERR_RANGE in the status word and is skipped.  Nothing but the rows' slots is written. */
+int cf_kv4_write(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t n_rows, const int64_t* slots,
+                 const void* k, const void* v, int64_t kv_layer_stride, int64_t row_stride, void* kv4,
+                 int64_t kv4_layer_stride, void* stream);
+
+/* The reverse: the numbers in the rows' slots, rounded to the storage type of geom (a request's rows for the kernels that take
+ * caches in the storage type, or for another pool).  Rows with a negative slot, and with one beyond the pool (CF_ERR_RANGE in
+ * the status word), stay as they are. */
+int cf_kv4_read(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t n_rows, const int64_t* slots,
+                const void* kv4, int64_t kv4_layer_stride, void* k, void* v, int64_t kv_layer_stride, int64_t row_stride,
+                void* stream);
+
+/* Scratch of cf_kv4_attn; 0 on invalid arguments. */
+size_t cf_kv4_attn_workspace_bytes(const cf_geom* geom, const cf_pages* pages, int32_t q_len, int32_t n_layers);
+
+/* Attention (Eq. 1) of q_len query tokens per request over its pages, whose last q_len rows are those tokens' own: query token
+ * j of request b sees rows 0 .. rows[b] - q_len + j (one token: all rows).  A query that sees no row gets zeros, and a log-sum-exp
+ * of -infinity; rows behind the last are not looked at.
+ *   q, out  device, storage type, [n_layers][n_requests][q_len][n_q_heads][head_dim], layers q_layer_stride / out_layer_stride
+ *           elements apart; queries and keys rotary-encoded at their own positions
+ *   kv4     the pool, layers kv4_layer_stride bytes apart
+ *   lse     device float [n_layers][n_requests][n_q_heads][q_len], natural log, or NULL
+ *   workspace  at least cf_kv4_attn_workspace_bytes(..., q_len, n_layers) bytes, 256-byte aligned; calls that share one must
+ *           not overlap on the device
+ * Keys and values enter the products exactly, queries of bf16 storage too; probabilities are rounded to 11 bits (fp32
+ * storage: queries and probabilities to 22), sums are fp32.  A table entry beyond the pool, or more rows than the table has
+ * room for, raises CF_ERR_RANGE in the status word; such a request's results mean nothing. */
+int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q,
+                int64_t q_layer_stride, const void* kv4, int64_t kv4_layer_stride, float softmax_scale, void* out,
+                int64_t out_layer_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* A batch of documents for the offline cache construction: a packed store like cf_batch's, without
  * requests, allocation or plan.  doc_offsets is DEVICE memory owned by the caller. */
 typedef struct cf_doc_batch {

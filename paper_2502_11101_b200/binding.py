@@ -34,11 +34,14 @@ EXPORTS = ["cf_error_string", "cf_allocate_positions", "cf_schedule_linear", "cf
            "cf_attn_workspace_bytes_full", "cf_query_prefill_attn_full", "cf_query_prefill_attn_prefix", "cf_assemble_final_cache", "cf_merge_attn",
            "cf_query_prefill_attn_static", "cf_prune_topk", "cf_prune_topk_host", "cf_run_stack_workspace_bytes",
            "cf_run_stack", "cf_document_prefill_attn", "cf_decode_plan_bytes", "cf_decode_plan", "cf_decode_status",
-           "cf_decode_workspace_bytes", "cf_decode_attn", "cf_decode_append", "cf_set_attn_path", "cf_profile_begin", "cf_profile_end", "cf_debug_wait_timeout",
+           "cf_decode_workspace_bytes", "cf_decode_attn", "cf_decode_append", "cf_pages_init",
+           "cf_pages_resize", "cf_pages_status", "cf_kv4_layer_bytes", "cf_kv4_write", "cf_kv4_read", "cf_kv4_attn_workspace_bytes",
+           "cf_kv4_attn", "cf_set_attn_path", "cf_profile_begin", "cf_profile_end", "cf_debug_wait_timeout",
            "cf_debug_attn_kernel", "cf_debug_cut_row"]
 _SIZE_T_EXPORTS = ("cf_attn_workspace_bytes", "cf_attn_workspace_bytes_layers", "cf_attn_workspace_bytes_full",
                    "cf_attn_workspace_bytes_slots", "cf_attn_workspace_bytes_slots_full",
-                   "cf_run_stack_workspace_bytes", "cf_decode_plan_bytes", "cf_decode_workspace_bytes")
+                   "cf_run_stack_workspace_bytes", "cf_decode_plan_bytes", "cf_decode_workspace_bytes", "cf_kv4_layer_bytes",
+                   "cf_kv4_attn_workspace_bytes")
 
 
 class cf_geom(ctypes.Structure):
@@ -67,6 +70,12 @@ class cf_doc_batch(ctypes.Structure):
     _fields_ = [("n_docs", ctypes.c_int32), ("max_doc_len", ctypes.c_int32), ("prefix_len", ctypes.c_int32),
                 ("reserved", ctypes.c_int32), ("total_tokens", ctypes.c_int64), ("token_stride", ctypes.c_int64),
                 ("doc_offsets", ctypes.c_void_p)]
+
+
+class cf_pages(ctypes.Structure):
+    _fields_ = [("n_requests", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("table_cols", ctypes.c_int32),
+                ("table", ctypes.c_void_p), ("rows", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
+                ("free_count", ctypes.c_void_p), ("status", ctypes.c_void_p)]
 
 
 class cf_stack(ctypes.Structure):
@@ -161,6 +170,17 @@ def load_library() -> ctypes.CDLL:
     lib.cf_decode_attn.argtypes = [gp, i32, i32, vp, i32, vp, i64, vp, vp, i64, ctypes.c_float, vp, i64, vp, vp,
                                    ctypes.c_size_t, vp]
     lib.cf_decode_append.argtypes = [gp, i32, i32, i32, vp, vp, i64, vp, i32, vp, vp, i64, vp, vp]
+    pp = ctypes.POINTER(cf_pages)
+    lib.cf_pages_init.argtypes = [pp, vp]
+    lib.cf_pages_resize.argtypes = [pp, vp, i32, i32, vp, vp]
+    lib.cf_pages_status.argtypes = [pp, vp]
+    lib.cf_kv4_layer_bytes.restype = ctypes.c_size_t
+    lib.cf_kv4_layer_bytes.argtypes = [gp, pp]
+    lib.cf_kv4_write.argtypes = [gp, pp, i32, i32, vp, vp, vp, i64, i64, vp, i64, vp]
+    lib.cf_kv4_read.argtypes = [gp, pp, i32, i32, vp, vp, i64, vp, vp, i64, i64, vp]
+    lib.cf_kv4_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.cf_kv4_attn_workspace_bytes.argtypes = [gp, pp, i32, i32]
+    lib.cf_kv4_attn.argtypes = [gp, pp, i32, i32, vp, i64, vp, i64, ctypes.c_float, vp, i64, vp, vp, ctypes.c_size_t, vp]
     lib.cf_set_attn_path.argtypes = [i32]
     lib.cf_profile_begin.argtypes = [i32]
     lib.cf_profile_end.argtypes = [vp, i32, vp]
@@ -604,6 +624,59 @@ def cf_decode_append(geom: cf_geom, n_requests: int, cache_rows: int, k_final: t
     """k_new, v_new [n_layers, B, Hkv, D] become row rows[b] + step of request b's slot in every layer."""
     _check(_native().decode_append(geom, n_requests, cache_rows, k_final, v_final, rows, step, k_new, v_new, status, stream),
            "cf_decode_append")
+
+
+def make_pages(table: torch.Tensor, rows: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor, status: torch.Tensor,
+               page_rows: int) -> cf_pages:
+    """The pages of a batch of requests: int32 device tensors the caller keeps alive, `table` [B, columns], `rows` [B],
+    `free_pages` [pages of the pool], `free_count` [1], `status` [1].  cf_pages_init sets them up."""
+    for t in (table, rows, free_pages, free_count, status):
+        assert t.dtype == torch.int32 and t.is_contiguous() and t.device == table.device
+    assert table.dim() == 2 and rows.shape == (table.shape[0],) and free_count.numel() == 1 and status.numel() == 1
+    return cf_pages(table.shape[0], page_rows, free_pages.numel(), table.shape[1], table.data_ptr(), rows.data_ptr(),
+                    free_pages.data_ptr(), free_count.data_ptr(), status.data_ptr())
+
+
+def cf_pages_init(pages: cf_pages, stream=None) -> None:
+    _check(load_library().cf_pages_init(ctypes.byref(pages), _stream(stream)), "cf_pages_init")
+
+
+def cf_pages_resize(pages: cf_pages, rows: torch.Tensor, extra_rows: int = 0, slots: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Request b is to have rows[b] + extra_rows rows (int32 [B]; none where rows[b] is negative); `slots` int64 [B, max_new]
+    receives the slots of the new ones."""
+    _check(_native().pages_resize(pages, rows, extra_rows, slots, stream), "cf_pages_resize")
+
+
+def cf_pages_status(pages: cf_pages, stream=None) -> int:
+    return int(load_library().cf_pages_status(ctypes.byref(pages), _stream(stream)))
+
+
+def cf_kv4_layer_bytes(geom: cf_geom, pages: cf_pages) -> int:
+    return int(load_library().cf_kv4_layer_bytes(ctypes.byref(geom), ctypes.byref(pages)))
+
+
+def cf_kv4_write(geom: cf_geom, pages: cf_pages, kv4: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                 stream=None) -> None:
+    """Rows k, v [n_layers, ..., Hkv, D] into `slots` (int64, one per row of a layer, negative: nowhere) of the pool kv4 (uint8
+    [n_layers, ...], a layer dense).  Rows may be padded; the dimensions between layers and heads lie one behind the other."""
+    _check(_native().kv4_write(geom, pages, kv4, slots, k, v, stream), "cf_kv4_write")
+
+
+def cf_kv4_read(geom: cf_geom, pages: cf_pages, kv4: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                stream=None) -> None:
+    """The reverse of cf_kv4_write: the numbers in `slots` into the rows of k and v."""
+    _check(_native().kv4_read(geom, pages, kv4, slots, k, v, stream), "cf_kv4_read")
+
+
+def cf_kv4_attn_workspace_bytes(geom: cf_geom, pages: cf_pages, q_len: int, n_layers: int) -> int:
+    return int(load_library().cf_kv4_attn_workspace_bytes(ctypes.byref(geom), ctypes.byref(pages), q_len, n_layers))
+
+
+def cf_kv4_attn(geom: cf_geom, pages: cf_pages, kv4: torch.Tensor, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                lse: Optional[torch.Tensor] = None, softmax_scale: float = 0.0, stream=None) -> None:
+    """q, out [n_layers, B, q_len, Hq, D]; kv4 uint8 [n_layers, ...], a layer dense; lse [n_layers, B, Hq, q_len].  Dimension 0 may
+    be strided."""
+    _check(_native().kv4_attn(geom, pages, kv4, q, out, workspace, lse, softmax_scale, stream), "cf_kv4_attn")
 
 
 def plan_field(plan: torch.Tensor, layout: cf_plan_layout, name: str, count: int, dtype=torch.int32) -> torch.Tensor:

@@ -347,6 +347,117 @@ NATIVE(decode_append) {                            // geom, n_requests, cache_ro
     });
 }
 
+// Whether what lies behind dimension 0 is dense.
+bool dense_layers(const at::Tensor& t) {
+    int64_t n = 1;
+    for (int64_t d = t.dim() - 1; d > 0; --d) {
+        if (t.size(d) != 1 && t.stride(d) != n) return false;
+        n *= t.size(d);
+    }
+    return true;
+}
+
+NATIVE(pages_resize) {                             // pages, rows, extra_rows, slots, stream
+    return guarded([&] {
+        Args in(argv, argc);
+        Bytes bp;
+        const cf_pages* p = in.structure<cf_pages>(bp);
+        const at::Tensor& rows = in.tensor();
+        const int32_t extra = in.i32();
+        const at::Tensor* slots = in.maybe_tensor();
+        void* s = in.stream();
+        require(rows.scalar_type() == at::kInt && rows.is_contiguous() && rows.numel() == p->n_requests, "rows: int32, one per request");
+        require(!slots || (slots->scalar_type() == at::kLong && slots->is_contiguous() && slots->numel() % p->n_requests == 0),
+                "slots: int64, as many for each request");
+        const int64_t room = slots ? slots->numel() / p->n_requests : 0;
+        require(room <= INT32_MAX, "slots: too many");
+        const int32_t* rp = (const int32_t*)rows.data_ptr();
+        int64_t* sp = slots ? (int64_t*)slots->data_ptr() : nullptr;
+        return call([&] { return cf_pages_resize(p, rp, extra, (int32_t)room, sp, s); });
+    });
+}
+
+// Rows of k and v for the calls on the 4-bit pool: [layers, rows ..., heads, dims], rows one behind the other.
+struct RowSpan {
+    int64_t layers, rows, layer_stride, row_stride;
+};
+RowSpan row_span(const cf_geom* g, const at::Tensor& kv4, const at::Tensor& slots, const at::Tensor& k, const at::Tensor& v) {
+    const int64_t size = g->dtype == CF_BF16 ? 2 : 4, nd = k.dim();
+    require(nd >= 4 && k.sizes() == v.sizes() && k.strides() == v.strides(), "k and v: one shape and stride");
+    require((int64_t)k.element_size() == size && (int64_t)v.element_size() == size, "k and v: the storage type of the geometry");
+    require(k.size(nd - 2) == g->n_kv_heads && k.size(nd - 1) == g->head_dim, "k and v: [layers, rows ..., heads, dims]");
+    require(k.stride(nd - 1) == 1 && k.stride(nd - 2) == g->head_dim, "k and v: a row is dense");
+    RowSpan r = {k.size(0), 1, k.stride(0), k.stride(nd - 3)};
+    for (int64_t d = nd - 3; d > 0; --d) {
+        require(k.size(d) == 1 || k.stride(d) == r.row_stride * r.rows, "k and v: rows lie one behind the other");
+        r.rows *= k.size(d);
+    }
+    if (r.rows <= 1) r.row_stride = (int64_t)g->n_kv_heads * g->head_dim;
+    require(r.rows <= INT32_MAX && r.layers <= INT32_MAX, "k and v: too many rows");
+    require(slots.scalar_type() == at::kLong && slots.is_contiguous() && slots.numel() == r.rows, "slots: int64, one per row of a layer");
+    require(kv4.scalar_type() == at::kByte && kv4.size(0) == r.layers, "kv4: bytes of as many layers");
+    return r;
+}
+
+NATIVE(kv4_write) {                                // geom, pages, kv4, slots, k, v, stream
+    return guarded([&] {
+        Args in(argv, argc);
+        Bytes bg, bp;
+        const cf_geom* g = in.structure<cf_geom>(bg);
+        const cf_pages* p = in.structure<cf_pages>(bp);
+        const at::Tensor &kv4 = in.tensor(), &slots = in.tensor(), &k = in.tensor(), &v = in.tensor();
+        void* s = in.stream();
+        const RowSpan r = row_span(g, kv4, slots, k, v);
+        const int64_t* sp = (const int64_t*)slots.data_ptr();
+        void *kp = k.data_ptr(), *vp = v.data_ptr(), *pool = kv4.data_ptr();
+        const int64_t ps = kv4.stride(0);
+        return call([&] { return cf_kv4_write(g, p, (int32_t)r.layers, (int32_t)r.rows, sp, kp, vp, r.layer_stride, r.row_stride, pool, ps, s); });
+    });
+}
+
+NATIVE(kv4_read) {                                 // geom, pages, kv4, slots, k, v, stream
+    return guarded([&] {
+        Args in(argv, argc);
+        Bytes bg, bp;
+        const cf_geom* g = in.structure<cf_geom>(bg);
+        const cf_pages* p = in.structure<cf_pages>(bp);
+        const at::Tensor &kv4 = in.tensor(), &slots = in.tensor(), &k = in.tensor(), &v = in.tensor();
+        void* s = in.stream();
+        const RowSpan r = row_span(g, kv4, slots, k, v);
+        const int64_t* sp = (const int64_t*)slots.data_ptr();
+        void *kp = k.data_ptr(), *vp = v.data_ptr(), *pool = kv4.data_ptr();
+        const int64_t ps = kv4.stride(0);
+        return call([&] { return cf_kv4_read(g, p, (int32_t)r.layers, (int32_t)r.rows, sp, pool, ps, kp, vp, r.layer_stride, r.row_stride, s); });
+    });
+}
+
+NATIVE(kv4_attn) {                                 // geom, pages, kv4, q, out, workspace, lse, scale, stream
+    return guarded([&] {
+        Args in(argv, argc);
+        Bytes bg, bp;
+        const cf_geom* g = in.structure<cf_geom>(bg);
+        const cf_pages* p = in.structure<cf_pages>(bp);
+        const at::Tensor &kv4 = in.tensor(), &q = in.tensor(), &out = in.tensor(), &ws = in.tensor();
+        const at::Tensor* lse = in.maybe_tensor();
+        const float scale = in.real();
+        void* s = in.stream();
+        const int64_t size = g->dtype == CF_BF16 ? 2 : 4;
+        require(q.dim() == 5 && out.sizes() == q.sizes() && dense_layers(q) && dense_layers(out), "q and out: [layers, requests, tokens, heads, dims]");
+        require((int64_t)q.element_size() == size && (int64_t)out.element_size() == size, "q and out: the storage type of the geometry");
+        require(q.size(1) == p->n_requests && q.size(3) == g->n_q_heads && q.size(4) == g->head_dim, "q: of other sizes than the geometry and the pages");
+        require(!lse || (lse->scalar_type() == at::kFloat && lse->is_contiguous() && lse->numel() == q.numel() / g->head_dim),
+                "lse: fp32, one per query and head");
+        require(kv4.scalar_type() == at::kByte && kv4.size(0) == q.size(0), "kv4: bytes of as many layers");
+        require(q.size(0) <= INT32_MAX && q.size(2) <= INT32_MAX, "q: too many layers or tokens");
+        const int32_t n = (int32_t)q.size(0), tokens = (int32_t)q.size(2);
+        const int64_t qs = q.stride(0), os = out.stride(0), ps = kv4.stride(0);
+        void *qp = q.data_ptr(), *op = out.data_ptr(), *pool = kv4.data_ptr(), *w = ws.data_ptr();
+        float* lp = lse ? (float*)lse->data_ptr() : nullptr;
+        const size_t wn = bytes_of(ws);
+        return call([&] { return cf_kv4_attn(g, p, n, tokens, qp, qs, pool, ps, scale, op, os, lp, w, wn, s); });
+    });
+}
+
 // A whole stack: geom, batch, plan, workspace, q, k, v, out, score_accum, schedule [(layer, keep), ...], strategy,
 // batch_layers, lse, layer_scores, k_final, k_self, v_self, scale, doc_len, req_doc_begin (int32 arrays or None),
 // k_prefix, v_prefix, stream.  Returns (code, 0), or (0, bytes) without doing anything when the workspace is smaller
@@ -442,7 +553,7 @@ NATIVE(run_stack) {
 PyMethodDef methods[] = {ENTRY(plan_init), ENTRY(prune_topk), ENTRY(reposition_keys), ENTRY(query_prefill_attn),
                          ENTRY(query_prefill_attn_slot), ENTRY(accumulate_scores), ENTRY(assemble_final_cache),
                          ENTRY(document_prefill_attn), ENTRY(decode_plan), ENTRY(decode_attn), ENTRY(decode_append),
-                         ENTRY(run_stack), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(pages_resize), ENTRY(kv4_write), ENTRY(kv4_read), ENTRY(kv4_attn), ENTRY(run_stack), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling of the hot calls", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,781 @@
+// Attention over the paged cache held in 4 bits (cf_kv4_attn).
+//
+//   out = sum_i p_i v_i / sum_i p_i,  p_i = 2^(x_i - m),  x_i = (q . k_i) * scale * log2(e),  k_i = s_k[i][j] c_k,  v_i = s_v[i][j] c_v
+// with one scale s per group j of 32 dims and codes c of 4 bits, 4.5 bits per number: a quarter of the bytes of a bf16 cache, and
+// 2 to 60 flops per byte, so the pass is bound by HBM as long as turning codes into matrix operands costs little.
+//   S^T = K Q^T   m16n8k16, rows = 16 keys, columns = 8 queries.  The codes go into the products as they are (fp16 holds
+//                 them exactly; the conversion gives two numbers an instruction); each group's partial sums are
+//                 multiplied by its scale in fp32, four multiply-adds per lane and group.  Queries are scaled by a power of two
+//                 per row so that bf16 fits fp16: the products are exact.
+//   O^T += V^T P^T  rows = dims, columns = queries, contraction over the keys.  The values' scales go into the
+//                 probabilities, one set per group: P_j = p * s_v[.][j] in fp32, rounded to fp16 (11 bits), under a power of two
+//                 that follows the largest scale seen, and transposed between the lanes by movmatrix.  Codes of two keys are
+//                 paired by bit operations, so that one conversion gives a register of the fragment.
+// Storage in fp32 splits queries and probabilities into two fp16 numbers each (22 bits) and issues every product twice.
+// The running maximum is raised only when a logit lies more than 2^8 above it: fp16 has room for that, and the
+// test is one vote of the warp.
+//
+// A block of 16 rows (2304 bytes at head_dim 128) comes by one bulk copy into a ring that belongs to the warp: no barrier
+// between warps, and 129 KB in flight per SM.  The blocks of all units (layer, request, kv head, tile of query columns)
+// lie end to end on one line, which is cut into equal shares; lengths are device data, so every warp finds its place by
+// walking the requests' lengths.  A share belongs to a warp where there are many units, else to the eight warps of a CTA, which
+// take its blocks in turn and join their results in shared memory.  Units cut between shares leave parts in the workspace, which
+// kv4_merge_kernel joins.
+#include <algorithm>
+#include <climits>
+
+#include "cf_kv4.cuh"
+#include "cf_tc_util.cuh"
+
+namespace cf {
+
+using namespace kv4;
+using tc::mbar_init;
+using tc::mbar_expect_tx;
+using tc::smem_u32;
+
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kStages = 4;
+constexpr int kMergeThreads = 256;
+constexpr float kSlack = 8.f;                     // how far a logit may lie above the running maximum (base 2)
+constexpr int kHead = 7;                          // P is at most 2^kSlack * 2^kHead, below fp16's 2^16
+constexpr int kLeastExponent = -110;
+
+struct Kv4Args {
+    const void* q;
+    const unsigned char* kv4;
+    void* out;
+    float* lse;
+    float* part_o;                                // [2 shares][columns][D]
+    float* part_ml;                               // [2 shares][2][columns]
+    int4* marks;                                  // [shares] what a share leaves for the merge: parts, layer, request, head * tiles + tile
+    long long q_layer_stride, kv4_layer_stride, out_layer_stride;
+    int n_layers, q_len, n_q_heads, n_kv_heads, group, columns, tiles;     // columns = group * q_len of a kv head
+    int n_shares, warps_per_share;
+    long long least_share;
+    float scale_log2;
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// What fp16 leaves of lo and hi.
+__device__ __forceinline__ uint32_t pack_f16_rest(float lo, float hi, uint32_t packed) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&packed));
+    return pack_f16(lo - f.x, hi - f.y);
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+    uint32_t x;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(a));
+    return x;
+}
+template <int N> __device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N]) {
+    static_assert(N == 1 || N == 2 || N == 4, "words of one load");
+    if constexpr (N == 1) w[0] = lds32(a);
+    if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a));
+    if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
+}
+
+__device__ __forceinline__ int steps_of(int rows) { return max(1, (rows + kBlockRows - 1) / kBlockRows); }
+
+// A place on the line: a unit and a block of it.
+struct Place {
+    int layer, request, unit;                     // unit = kv head * tiles + tile, within (layer, request)
+    int rows, steps;                              // of the request
+    int step;
+};
+
+// Steps of all requests, and the place `at` steps along the line (units of a request are neighbours, layers outermost).
+struct Line {
+    const PagesView& pv;
+    int units;                                    // per (layer, request)
+    int most;                                     // rows the table has room for
+    __device__ __forceinline__ int rows_of(int b) const { return min(max(pv.rows[b], 0), most); }
+    __device__ __forceinline__ long long steps_of_layer() const {
+        long long sum = 0;
+        for (int b = threadIdx.x & 31; b < pv.n_requests; b += 32) sum += steps_of(rows_of(b));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        return sum * units;
+    }
+    __device__ __forceinline__ Place find(long long at, long long per_layer) const {
+        const int lane = threadIdx.x & 31;
+        Place p = {};
+        if (at >= per_layer) p.layer = (int)(at / per_layer), at -= p.layer * per_layer;
+        for (int b0 = 0;; b0 += 32) {
+            const int b = b0 + lane, rows = b < pv.n_requests ? rows_of(b) : 0, steps = b < pv.n_requests ? steps_of(rows) : 0;
+            long long end = (long long)steps * units;
+            const long long mine = end;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long x = __shfl_up_sync(0xffffffffu, end, o);
+                if (lane >= o) end += x;
+            }
+            const unsigned behind = __ballot_sync(0xffffffffu, end > at);
+            if (behind != 0 || b0 + 32 >= pv.n_requests) {
+                const int src = behind != 0 ? __ffs(behind) - 1 : 0;
+                p.request = b0 + src;
+                p.rows = __shfl_sync(0xffffffffu, rows, src);
+                p.steps = __shfl_sync(0xffffffffu, steps, src);
+                const int within = (int)(at - __shfl_sync(0xffffffffu, end - mine, src));    // units * steps: below 2^31 for every cache that fits
+                p.unit = within / p.steps;
+                p.step = within - p.unit * p.steps;
+                return p;
+            }
+            at -= __shfl_sync(0xffffffffu, end, 31);
+        }
+    }
+    __device__ __forceinline__ void next_unit(Place& p) const {
+        p.step = 0;
+        if (++p.unit < units) return;
+        p.unit = 0;
+        if (++p.request == pv.n_requests) p.request = 0, ++p.layer;
+        p.rows = rows_of(p.request);
+        p.steps = steps_of(p.rows);
+    }
+};
+
+// The copies of a warp's blocks: it takes every stride-th block from `first` on of each unit of its share.
+template <int D>
+struct Feeder {
+    static constexpr int kBytes = block_bytes(D);
+    const PagesView& pv;
+    const Kv4Args& a;
+    const Line& line;
+    Divisor blocks_per_page;
+    Place p;
+    long long left;                               // steps of the share from the beginning of p's unit (from p.step) on
+    int first, stride;
+    int ready, used;                              // blocks whose addresses the lanes hold; blocks of them that were issued
+    const unsigned char* address;                 // lane l's block
+    int base;                                     // next step of the unit to look up
+    uint32_t ring, bars;
+    int stage;
+    unsigned issued;
+
+    // The next up to 32 blocks: every lane looks one up.
+    __device__ __forceinline__ void look_up() {
+        const int lane = threadIdx.x & 31;
+        while (true) {
+            const int end = (int)min((long long)p.steps, p.step + left);
+            const int n = base < end ? (end - base + stride - 1) / stride : 0;
+            if (n > 0) {
+                ready = min(32, n);
+                used = 0;
+                address = nullptr;
+                if (lane < ready) {
+                    const int step = base + lane * stride;
+                    const int column = blocks_per_page.quotient(step);
+                    int page = pv.table[(size_t)p.request * pv.table_cols + column];
+                    if ((unsigned)page >= (unsigned)pv.n_pages) {
+                        if (p.rows > 0) atomicCAS(pv.status, 0, CF_ERR_RANGE);   // a request without rows has no pages
+                        page = 0;
+                    }
+                    const int head = p.unit / a.tiles;
+                    address = a.kv4 + (size_t)p.layer * a.kv4_layer_stride +
+                              (((size_t)page * a.n_kv_heads + head) * blocks_per_page.d + (step - column * (int)blocks_per_page.d)) * kBytes;
+                }
+                base += ready * stride;
+                return;
+            }
+            left -= end - p.step;
+            if (left <= 0) {
+                ready = used = 0;
+                return;
+            }
+            line.next_unit(p);
+            base = first;
+        }
+    }
+    // Issues the next block's copy into the stage that was read last.
+    __device__ __forceinline__ void feed() {
+        if (used == ready) {
+            if (ready == 0) return;
+            look_up();
+            if (ready == 0) return;
+        }
+        if ((int)(threadIdx.x & 31) == used) {
+            const uint32_t bar = bars + 8 * stage;
+            mbar_expect_tx(bar, kBytes);
+            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ring + stage * kBytes),
+                         "l"(address), "r"(kBytes), "r"(bar)
+                         : "memory");
+        }
+        ++used;
+        ++issued;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
+    }
+};
+
+template <typename T> struct IsF32 { static constexpr bool value = sizeof(T) == 4; };
+
+template <typename T>
+__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d);
+template <>
+__device__ __forceinline__ void store4<float>(float* p, float a, float b, float c, float d) {
+    *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
+}
+template <>
+__device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, float a, float b, float c, float d) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b), y = __floats2bfloat162_rn(c, d);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+}
+
+// Results of a column: where they go, by the column's number within the kv head (token-major).
+template <typename T, int D>
+__device__ __forceinline__ T* out_row(const Kv4Args& a, int n_requests, int layer, int request, int head, int column) {
+    const int token = column / a.group, h = head * a.group + column % a.group;
+    return static_cast<T*>(a.out) + (size_t)layer * a.out_layer_stride + (((size_t)request * a.q_len + token) * a.n_q_heads + h) * D;
+}
+__device__ __forceinline__ void store_lse(const Kv4Args& a, int n_requests, int layer, int request, int head, int column, float m, float l) {
+    if (!a.lse) return;
+    const int token = column / a.group, h = head * a.group + column % a.group;
+    a.lse[(((size_t)layer * n_requests + request) * a.n_q_heads + h) * a.q_len + token] = l > 0.f || l != l ? m * kLn2 + logf(l) : -INFINITY;
+}
+
+template <typename T, int D, int NT>
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
+kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
+    chain_next();
+    constexpr int kBytes = block_bytes(D);
+    constexpr int kGroups = D / 32;
+    constexpr int kCols = 8 * NT;
+    constexpr int kParts = IsF32<T>::value ? 2 : 1;          // fp16 numbers per query or probability
+    constexpr int kOStride = D + 4;                          // floats between columns in shared memory: no bank conflicts
+    extern __shared__ __align__(128) unsigned char smem[];
+    unsigned char* s_ring = smem;                            // [kWarps][kStages][kBytes]
+    float* s_o = reinterpret_cast<float*>(smem + kWarps * kStages * kBytes);    // [kWarps][kCols][kOStride]
+    float* s_m = s_o + kWarps * kCols * kOStride;            // [kWarps][kCols]
+    float* s_l = s_m + kWarps * kCols;                       // [kWarps][kCols]
+    unsigned long long* s_bars = reinterpret_cast<unsigned long long*>(s_l + kWarps * kCols);   // [kWarps][kStages]
+    __shared__ volatile int s_abort;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    if (lane < kStages) mbar_init(smem_u32(s_bars + warp * kStages + lane), 1);
+    if (tid == 0) s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    __syncthreads();
+    chain_wait();
+    const Kv4Args& a = args;
+    asm volatile("fence.proxy.async;" ::: "memory");         // what earlier kernels wrote is read by bulk copies
+
+    const bool together = a.warps_per_share > 1;             // the CTA's warps share a share
+    const int share = together ? (int)blockIdx.x : (int)blockIdx.x * kWarps + warp;
+    const Line line = {pv, a.n_kv_heads * a.tiles, pv.table_cols * pv.page_rows};
+    const long long per_layer = line.steps_of_layer(), total = per_layer * a.n_layers;
+    const long long size = max(a.least_share, (total + a.n_shares - 1) / a.n_shares);
+    const long long begin = share * size;
+    long long left = min(size, total - begin);
+    if (lane == 0 && (!together || warp == 0)) a.marks[share] = make_int4(0, 0, 0, 0);
+    if (share == 0 && (!together || warp == 0))
+        for (int b = lane; b < pv.n_requests; b += 32)
+            if (pv.rows[b] < 0 || pv.rows[b] > line.most) atomicCAS(pv.status, 0, CF_ERR_RANGE);
+    if (left <= 0) return;                                   // a warp's or the whole CTA's, no barrier follows
+
+    Place p = line.find(begin, per_layer);
+    const int first_step = together ? warp : 0, stride = together ? kWarps : 1;
+    const uint32_t ring = smem_u32(s_ring) + warp * kStages * kBytes, bars = smem_u32(s_bars + warp * kStages);
+    Feeder<D> feeder = {pv, a, line, blocks_per_page, p, left, first_step, stride, 0, 0, nullptr, p.step + first_step, ring, bars, 0, 0u};
+    feeder.look_up();
+#pragma unroll
+    for (int i = 0; i < kStages; ++i) feeder.feed();
+    int stage = 0, phase = 0;
+    unsigned taken = 0;                                      // copies that were waited for
+    bool given_up = false;
+    bool whole_start = p.step == 0;                          // the share's part of the unit begins with the unit
+
+    while (left > 0) {                                       // a unit, or the share's part of one
+        const int end = (int)min((long long)p.steps, p.step + left);
+        const int head = p.unit / a.tiles, col0 = (p.unit - head * a.tiles) * kCols;
+        // the queries: lane (g, t) holds dims 32 j + 8 t .. + 7 of column g of every tile of eight
+        uint32_t qf[NT][kParts][kGroups][2][2];
+        float cs[NT][2];                                     // what turns sums of codes into base-2 logits, columns 2t and 2t + 1
+        int sees[NT][2];                                     // rows that they see
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int column = col0 + 8 * n + g;
+            float x[kGroups][8];
+            uint32_t amax = 0;
+            if (column < a.columns) {
+                const int token = column / a.group, h = head * a.group + column % a.group;
+                const T* q = static_cast<const T*>(a.q) + (size_t)p.layer * a.q_layer_stride + (((size_t)p.request * a.q_len + token) * a.n_q_heads + h) * D + 8 * t;
+#pragma unroll
+                for (int j = 0; j < kGroups; ++j) {
+                    uint32_t w[4 * kParts];
+#pragma unroll
+                    for (int i = 0; i < kParts; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = *reinterpret_cast<const uint4*>(q + 32 * j + 4 * i);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        x[j][i] = IsF32<T>::value ? __uint_as_float(w[i % (4 * kParts)]) : i & 1 ? bf16_high(w[i / 2]) : bf16_low(w[i / 2]);
+                        amax = max(amax, __float_as_uint(x[j][i]) & 0x7fffffffu);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
+            }
+            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
+            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+            int e = amax == 0 || amax >= 0x7f800000u ? 0 : (int)(amax >> 23) - 127;      // the largest magnitude comes to lie in [1, 2)
+            e = max(-126, min(126, e));
+            const float down = __int_as_float((127 - e) << 23), up = __int_as_float((127 + e) << 23);
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float lo = x[j][2 * i] * down, hi = x[j][2 * i + 1] * down;
+                    qf[n][0][j][i / 2][i & 1] = pack_f16(lo, hi);
+                    if (kParts == 2) qf[n][kParts - 1][j][i / 2][i & 1] = pack_f16_rest(lo, hi, qf[n][0][j][i / 2][i & 1]);
+                }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                cs[n][i] = a.scale_log2 * __shfl_sync(0xffffffffu, up, (2 * t + i) * 4);
+                const int mine = col0 + 8 * n + 2 * t + i;
+                sees[n][i] = mine < a.columns ? p.rows - a.q_len + 1 + mine / a.group : p.rows;
+            }
+        }
+        const int all_see = p.rows - a.q_len + 1 + col0 / a.group;       // what the tile's first column sees, the fewest
+
+        float o[NT][kGroups][2][4], m[NT][2], l[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) o[n][j][i][k] = 0.f;
+            m[n][0] = m[n][1] = -INFINITY;
+            l[n][0] = l[n][1] = 0.f;
+        }
+        int exponent = kLeastExponent;                       // values are taken in units of 2^(exponent - kHead)
+        float scale_limit = __int_as_float((127 + exponent) << 23), scale_down = exp2f((float)(kHead - exponent));
+
+        for (int step = p.step + first_step; step < end; step += stride) {
+            const uint32_t block = ring + stage * kBytes;
+            if (!given_up && !tc::mbar_wait(bars + 8 * stage, phase, &s_abort)) given_up = true;
+            if (!given_up) ++taken;
+            // S^T of 16 keys
+            float s[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
+            {
+                uint32_t k0[kGroups], k1[kGroups], ks0[kGroups / 2], ks1[kGroups / 2];
+                lds<kGroups>(block + key_code_at<D>(g) + t * (D / 8), k0);
+                lds<kGroups>(block + key_code_at<D>(g + 8) + t * (D / 8), k1);
+                lds<kGroups / 2>(block + key_scale_at<D>(g), ks0);
+                lds<kGroups / 2>(block + key_scale_at<D>(g + 8), ks1);
+#pragma unroll
+                for (int j = 0; j < kGroups; ++j) {
+                    const uint32_t a00 = two_numbers<0>(k0[j]), a10 = two_numbers<0>(k1[j]), a20 = two_numbers<1>(k0[j]), a30 = two_numbers<1>(k1[j]);
+                    const uint32_t a01 = two_numbers<2>(k0[j]), a11 = two_numbers<2>(k1[j]), a21 = two_numbers<3>(k0[j]), a31 = two_numbers<3>(k1[j]);
+                    const float f0 = j & 1 ? bf16_high(ks0[j / 2]) : bf16_low(ks0[j / 2]), f1 = j & 1 ? bf16_high(ks1[j / 2]) : bf16_low(ks1[j / 2]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float c[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int i = 0; i < kParts; ++i) {
+                            mma_f16(c, a00, a10, a20, a30, qf[n][i][j][0][0], qf[n][i][j][0][1]);
+                            mma_f16(c, a01, a11, a21, a31, qf[n][i][j][1][0], qf[n][i][j][1][1]);
+                        }
+                        s[n][0] = fmaf(c[0], f0, s[n][0]), s[n][1] = fmaf(c[1], f0, s[n][1]);
+                        s[n][2] = fmaf(c[2], f1, s[n][2]), s[n][3] = fmaf(c[3], f1, s[n][3]);
+                    }
+                }
+            }
+            uint32_t vw[2][2][kGroups / 2];                  // [half][odd][groups two by two]
+            float vs[2][kGroups];                            // scales of keys g and g + 8
+            {
+                uint32_t w[kGroups], ws[kGroups / 2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    lds<kGroups>(block + value_code_at<D>(8 * h + 2 * t, g), w);
+#pragma unroll
+                    for (int i = 0; i < kGroups / 2; ++i) vw[h][0][i] = w[i], vw[h][1][i] = w[kGroups / 2 + i];
+                    lds<kGroups / 2>(block + value_scale_at<D>(g + 8 * h), ws);
+#pragma unroll
+                    for (int i = 0; i < kGroups / 2; ++i) vs[h][2 * i] = bf16_low(ws[i]), vs[h][2 * i + 1] = bf16_high(ws[i]);
+                }
+            }
+            __syncwarp();                                    // the stage has been read
+            if (!given_up) feeder.feed();
+            if (++stage == kStages) stage = 0, phase ^= 1;
+
+            const bool masked = (step + 1) * kBlockRows > all_see;
+            bool raise = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[n][i] *= cs[n][i & 1];
+                    if (masked && step * kBlockRows + g + 8 * (i >> 1) >= sees[n][i & 1]) s[n][i] = -INFINITY;
+                    raise |= s[n][i] > m[n][i & 1] + kSlack;
+                }
+            if (masked) {                                    // rows behind the last may hold anything
+                bool nan = false;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < kGroups; ++j) {
+                        if (step * kBlockRows + g + 8 * h >= p.rows) vs[h][j] = 0.f;
+                        nan |= vs[h][j] != vs[h][j];
+                    }
+                if (__any_sync(0xffffffffu, nan)) {          // reaches the queries that see the row, and no others
+#pragma unroll
+                    for (int j = 0; j < kGroups; ++j) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                bool hit = false;
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) hit |= vs[h][j] != vs[h][j] && step * kBlockRows + g + 8 * h < sees[n][i];
+                                // lanes of the same columns: bits t, t + 4, ...
+                                if (__ballot_sync(0xffffffffu, hit) & (0x11111111u << t))
+#pragma unroll
+                                    for (int k = 0; k < 2; ++k) o[n][j][k][i] = o[n][j][k][i + 2] = __int_as_float(0x7fffffff);
+                            }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            if (vs[h][j] != vs[h][j]) vs[h][j] = 0.f;
+                    }
+                }
+            }
+            float vmax = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < kGroups; ++j) vmax = fmaxf(vmax, vs[h][j]);
+            raise |= vmax > scale_limit;
+            if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, x));
+                float f = 1.f;
+                if (vmax > scale_limit) {
+                    const int e = min((int)(__float_as_uint(vmax) >> 23) - 126, 127);
+                    f = exp2f((float)(exponent - e));
+                    exponent = e;
+                    scale_limit = __int_as_float((127 + e) << 23);
+                    scale_down = exp2f((float)(kHead - e));
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float x = fmaxf(s[n][i], s[n][i + 2]);
+#pragma unroll
+                        for (int y = 4; y < 32; y <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, y));
+                        x = fmaxf(x, m[n][i]);
+                        const float r = x == m[n][i] ? 1.f : exp2_fast(m[n][i] - x);
+                        m[n][i] = x;
+                        l[n][i] *= r;
+#pragma unroll
+                        for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) o[n][j][k][i] *= r * f, o[n][j][k][i + 2] *= r * f;
+                    }
+            }
+            // the probabilities
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = exp2_fast(s[n][i] - m[n][i & 1]);
+                    if (masked && s[n][i] == -INFINITY) x = 0.f;
+                    l[n][i & 1] += x;
+                    s[n][i] = x * scale_down;
+                }
+            // O^T += V^T P^T, group by group
+#pragma unroll
+            for (int j = 0; j < kGroups; ++j) {
+                constexpr uint32_t kLow = 0x0f0f0f0fu;
+                uint32_t even[2], odd[2];                    // [half]: codes of an even dim of two keys to a byte; of an odd dim
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t w0 = vw[h][0][j / 2], w1 = vw[h][1][j / 2];
+                    even[h] = (w0 & kLow) | ((w1 << 4) & ~kLow);
+                    odd[h] = ((w0 >> 4) & kLow) | (w1 & ~kLow);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    uint32_t b[kParts][2];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float x = s[n][2 * h] * vs[h][j], y = s[n][2 * h + 1] * vs[h][j];
+                        const uint32_t w = pack_f16(x, y);
+                        b[0][h] = transposed(w);
+                        if (kParts == 2) b[kParts - 1][h] = transposed(pack_f16_rest(x, y, w));
+                    }
+#pragma unroll
+                    for (int i = 0; i < kParts; ++i) {
+                        if (j & 1) {
+                            mma_f16(o[n][j][0], two_numbers<2>(even[0]), two_numbers<2>(odd[0]), two_numbers<2>(even[1]), two_numbers<2>(odd[1]), b[i][0], b[i][1]);
+                            mma_f16(o[n][j][1], two_numbers<3>(even[0]), two_numbers<3>(odd[0]), two_numbers<3>(even[1]), two_numbers<3>(odd[1]), b[i][0], b[i][1]);
+                        } else {
+                            mma_f16(o[n][j][0], two_numbers<0>(even[0]), two_numbers<0>(odd[0]), two_numbers<0>(even[1]), two_numbers<0>(odd[1]), b[i][0], b[i][1]);
+                            mma_f16(o[n][j][1], two_numbers<1>(even[0]), two_numbers<1>(odd[0]), two_numbers<1>(even[1]), two_numbers<1>(odd[1]), b[i][0], b[i][1]);
+                        }
+                    }
+                }
+            }
+        }
+
+        // the unit is done, or as much of it as the share has
+        const float unit_scale = exp2f((float)(exponent - kHead));
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], x);
+        const bool whole = whole_start && end == p.steps;
+        const int slot = 2 * share + (whole_start ? 1 : 0);
+        if (together) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int c = 8 * n + 2 * t + i;
+                    float* row = s_o + (warp * kCols + c) * kOStride + 4 * g;
+#pragma unroll
+                    for (int j = 0; j < kGroups; ++j)
+                        *reinterpret_cast<float4*>(row + 32 * j) =
+                            make_float4(o[n][j][0][i] * unit_scale, o[n][j][0][i + 2] * unit_scale, o[n][j][1][i] * unit_scale, o[n][j][1][i + 2] * unit_scale);
+                    if (g == 0) s_m[warp * kCols + c] = m[n][i], s_l[warp * kCols + c] = l[n][i];
+                }
+            __syncthreads();
+            for (int i = tid; i < kCols * (D / 4); i += kThreads) {
+                const int c = i / (D / 4), d = i % (D / 4) * 4, column = col0 + c;
+                float top = -INFINITY;
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w * kCols + c]);
+                float sum = 0.f;
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    const float mw = s_m[w * kCols + c], f = mw == -INFINITY ? 0.f : exp2f(mw - top), lw = s_l[w * kCols + c];
+                    const float4 y = *reinterpret_cast<const float4*>(s_o + (w * kCols + c) * kOStride + d);
+                    // a warp that saw no key (or only NaN) has m = -inf
+                    if (mw == -INFINITY && lw == 0.f) continue;
+                    const float k = mw == -INFINITY ? 1.f : f;
+                    sum = fmaf(lw, k, sum);
+                    x.x = fmaf(y.x, k, x.x), x.y = fmaf(y.y, k, x.y), x.z = fmaf(y.z, k, x.z), x.w = fmaf(y.w, k, x.w);
+                }
+                if (whole) {
+                    if (column < a.columns) {
+                        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                        store4<T>(out_row<T, D>(a, pv.n_requests, p.layer, p.request, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+                        if (d == 0) store_lse(a, pv.n_requests, p.layer, p.request, head, column, top, sum);
+                    }
+                } else {
+                    *reinterpret_cast<float4*>(a.part_o + ((size_t)slot * kCols + c) * D + d) = x;
+                    if (d == 0) a.part_ml[(size_t)slot * 2 * kCols + c] = top, a.part_ml[(size_t)slot * 2 * kCols + kCols + c] = sum;
+                }
+            }
+            __syncthreads();
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int c = 8 * n + 2 * t + i, column = col0 + c;
+                    const float f = !whole ? unit_scale : l[n][i] == 0.f ? 0.f : unit_scale / l[n][i];
+                    if (whole) {
+                        if (column < a.columns) {
+                            T* row = out_row<T, D>(a, pv.n_requests, p.layer, p.request, head, column) + 4 * g;
+#pragma unroll
+                            for (int j = 0; j < kGroups; ++j)
+                                store4<T>(row + 32 * j, o[n][j][0][i] * f, o[n][j][0][i + 2] * f, o[n][j][1][i] * f, o[n][j][1][i + 2] * f);
+                            if (g == 0) store_lse(a, pv.n_requests, p.layer, p.request, head, column, m[n][i], l[n][i]);
+                        }
+                    } else {
+                        float* row = a.part_o + ((size_t)slot * kCols + c) * D + 4 * g;
+#pragma unroll
+                        for (int j = 0; j < kGroups; ++j)
+                            store4<float>(row + 32 * j, o[n][j][0][i] * f, o[n][j][0][i + 2] * f, o[n][j][1][i] * f, o[n][j][1][i + 2] * f);
+                        if (g == 0) a.part_ml[(size_t)slot * 2 * kCols + c] = m[n][i], a.part_ml[(size_t)slot * 2 * kCols + kCols + c] = l[n][i];
+                    }
+                }
+        }
+        if (whole_start && !whole && lane == 0 && (!together || warp == 0)) {
+            const long long more = p.steps - end;             // blocks of the unit in later shares
+            a.marks[share] = make_int4(1 + (int)((more + size - 1) / size), p.layer, p.request, p.unit);
+        }
+        left -= end - p.step;
+        if (left > 0) line.next_unit(p);
+        whole_start = true;
+    }
+    if (given_up) {                                          // its copies in flight are given the time to end
+        for (; taken < feeder.issued; ++taken) {
+            const long long t0 = clock64();
+            while (!tc::mbar_try_wait(bars + 8 * (taken % kStages), taken / kStages & 1) && clock64() - t0 < tc::kWaitLimitCycles) {}
+        }
+        if (lane == 0) atomicCAS(pv.status, 0, CF_ERR_TIMEOUT);
+    }
+}
+
+// Joins the parts of the unit that begins in share blockIdx.x and goes on in later ones.
+template <typename T, int D>
+__global__ void __launch_bounds__(kMergeThreads)
+kv4_merge_kernel(Kv4Args a, PagesView pv, int cols) {
+    chain_next();
+    chain_wait();
+    const int share = blockIdx.x;
+    const int4 mark = a.marks[share];
+    if (mark.x > 0) {
+        const int head = mark.w / a.tiles, col0 = (mark.w - head * a.tiles) * cols;
+        for (int i = threadIdx.x; i < cols * (D / 4); i += kMergeThreads) {
+            const int c = i / (D / 4), d = i % (D / 4) * 4, column = col0 + c;
+            if (column >= a.columns) continue;
+            float top = -INFINITY, sum = 0.f;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int k = 0; k < mark.x; ++k) {
+                const size_t slot = k == 0 ? 2 * (size_t)share + 1 : 2 * (size_t)(share + k);
+                const float m = a.part_ml[slot * 2 * cols + c], l = a.part_ml[slot * 2 * cols + cols + c];
+                const float4 y = *reinterpret_cast<const float4*>(a.part_o + (slot * cols + c) * D + d);
+                if (m == -INFINITY && l == 0.f) continue;
+                const float to = fmaxf(top, m), f0 = top == to ? 1.f : exp2f(top - to), f1 = m == to || m == -INFINITY ? 1.f : exp2f(m - to);
+                sum = fmaf(sum, f0, l * f1);
+                x.x = fmaf(x.x, f0, y.x * f1), x.y = fmaf(x.y, f0, y.y * f1), x.z = fmaf(x.z, f0, y.z * f1), x.w = fmaf(x.w, f0, y.w * f1);
+                top = to;
+            }
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            store4<T>(out_row<T, D>(a, pv.n_requests, mark.y, mark.z, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+            if (d == 0) store_lse(a, pv.n_requests, mark.y, mark.z, head, column, top, sum);
+        }
+    }
+}
+
+// How a call is cut: everything the host can know of it.
+struct Cut {
+    int nt;                                       // tiles of eight query columns that a warp takes
+    int tiles, columns;
+    int ctas, n_shares, warps_per_share;
+};
+
+Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
+    Cut c = {};
+    c.columns = g->n_q_heads / g->n_kv_heads * q_len;
+    c.nt = c.columns <= 8 ? 1 : 2;
+    c.tiles = (c.columns + 8 * c.nt - 1) / (8 * c.nt);
+    c.ctas = sm_count() * (c.nt == 1 ? 2 : 1);
+    const double units = (double)n_layers * p->n_requests * g->n_kv_heads * c.tiles;
+    c.warps_per_share = units >= 2.0 * c.ctas * kWarps ? 1 : kWarps;
+    c.n_shares = c.warps_per_share == 1 ? c.ctas * kWarps : c.ctas;
+    return c;
+}
+
+size_t round_up(size_t x) { return (x + 255) / 256 * 256; }
+
+int check_attn(const cf_geom* geom, const cf_pages* pages, int q_len, int n_layers) {
+    int rc = validate(geom, nullptr);
+    if (rc == CF_OK) rc = check_pages(pages);
+    if (rc != CF_OK) return rc;
+    if (q_len <= 0 || n_layers <= 0 || n_layers > 65535) return CF_ERR_INVALID_ARG;
+    const long long columns = (long long)geom->n_q_heads / geom->n_kv_heads * q_len;
+    const long long tiles = (columns + 7) / 8;
+    if (columns > (1 << 24) || tiles * geom->n_kv_heads * ((long long)pages->table_cols * (pages->page_rows / 16) + 1) > INT_MAX)
+        return CF_ERR_INVALID_ARG;                // a request's blocks are counted in 32 bits
+    return CF_OK;
+}
+
+size_t attn_smem(int head_dim, int nt) {
+    return (size_t)kWarps * kStages * block_bytes(head_dim) + (size_t)kWarps * 8 * nt * (head_dim + 4) * 4 + 2 * (size_t)kWarps * 8 * nt * 4 +
+           (size_t)kWarps * kStages * 8;
+}
+
+template <typename T, int D, int NT>
+int launch_attn(const Kv4Args& a, const PagesView& pv, Divisor blocks_per_page, int ctas, cudaStream_t stream) {
+    static PerDeviceOnce once;
+    const size_t smem = attn_smem(D, NT);
+    const int rc = configure_smem_once(once, kv4_attn_kernel<T, D, NT>, (int)smem);
+    if (rc != CF_OK) return rc;
+    const int err = launch_chained(kv4_attn_kernel<T, D, NT>, dim3((unsigned)ctas), kThreads, smem, stream, a, pv, blocks_per_page);
+    if (err != CF_OK) return err;
+    return launch_chained(kv4_merge_kernel<T, D>, dim3((unsigned)a.n_shares), kMergeThreads, 0, stream, a, pv, 8 * NT);
+}
+
+template <typename T>
+int launch_attn_typed(const Kv4Args& a, const PagesView& pv, Divisor blocks_per_page, const Cut& c, int head_dim, cudaStream_t stream) {
+    if (head_dim == 128)
+        return c.nt == 1 ? launch_attn<T, 128, 1>(a, pv, blocks_per_page, c.ctas, stream) : launch_attn<T, 128, 2>(a, pv, blocks_per_page, c.ctas, stream);
+    return c.nt == 1 ? launch_attn<T, 64, 1>(a, pv, blocks_per_page, c.ctas, stream) : launch_attn<T, 64, 2>(a, pv, blocks_per_page, c.ctas, stream);
+}
+
+}  // namespace
+
+}  // namespace cf
+
+using namespace cf;
+
+extern "C" {
+
+size_t cf_kv4_attn_workspace_bytes(const cf_geom* geom, const cf_pages* pages, int32_t q_len, int32_t n_layers) {
+    if (check_attn(geom, pages, q_len, n_layers) != CF_OK) return 0;
+    const Cut c = cut_of(geom, pages, q_len, n_layers);
+    const size_t rows = 2 * (size_t)c.n_shares * 8 * c.nt;
+    return round_up(rows * geom->head_dim * 4) + round_up(rows * 8) + round_up((size_t)c.n_shares * sizeof(int4));
+}
+
+int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q,
+                int64_t q_layer_stride, const void* kv4, int64_t kv4_layer_stride, float softmax_scale, void* out,
+                int64_t out_layer_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check_attn(geom, pages, q_len, n_layers);
+    if (rc != CF_OK) return rc;
+    if (!q || !kv4 || !out || !workspace) return CF_ERR_INVALID_ARG;
+    const int esize = geom->dtype == CF_BF16 ? 2 : 4;
+    for (const void* p : {q, kv4, static_cast<const void*>(out)})
+        if (reinterpret_cast<uintptr_t>(p) % 16) return CF_ERR_INVALID_ARG;
+    if ((q_layer_stride * esize) % 16 || (out_layer_stride * esize) % 16 || kv4_layer_stride % 16) return CF_ERR_INVALID_ARG;
+    const long long layer_elems = (long long)pages->n_requests * q_len * geom->n_q_heads * geom->head_dim;
+    if (n_layers > 1 && (q_layer_stride < layer_elems || out_layer_stride < layer_elems ||
+                         kv4_layer_stride < (long long)cf_kv4_layer_bytes(geom, pages)))
+        return CF_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < cf_kv4_attn_workspace_bytes(geom, pages, q_len, n_layers))
+        return CF_ERR_WORKSPACE;
+    const Cut c = cut_of(geom, pages, q_len, n_layers);
+    const float scale = softmax_scale != 0.f ? softmax_scale : 1.f / sqrtf((float)geom->head_dim);
+    const size_t rows = 2 * (size_t)c.n_shares * 8 * c.nt;
+    char* w = static_cast<char*>(workspace);
+    Kv4Args a = {};
+    a.q = q, a.kv4 = static_cast<const unsigned char*>(kv4), a.out = out, a.lse = lse;
+    a.part_o = reinterpret_cast<float*>(w);
+    a.part_ml = reinterpret_cast<float*>(w + round_up(rows * geom->head_dim * 4));
+    a.marks = reinterpret_cast<int4*>(w + round_up(rows * geom->head_dim * 4) + round_up(rows * 8));
+    a.q_layer_stride = q_layer_stride, a.kv4_layer_stride = kv4_layer_stride, a.out_layer_stride = out_layer_stride;
+    a.n_layers = n_layers, a.q_len = q_len, a.n_q_heads = geom->n_q_heads, a.n_kv_heads = geom->n_kv_heads;
+    a.group = geom->n_q_heads / geom->n_kv_heads, a.columns = c.columns, a.tiles = c.tiles;
+    a.n_shares = c.n_shares, a.warps_per_share = c.warps_per_share;
+    a.least_share = c.warps_per_share == 1 ? 4 : 2 * kWarps;
+    a.scale_log2 = scale * kLog2e;
+    const PagesView pv = make_pages_view(pages);
+    const Divisor blocks_per_page(pages->page_rows / kBlockRows);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return geom->dtype == CF_BF16 ? launch_attn_typed<__nv_bfloat16>(a, pv, blocks_per_page, c, geom->head_dim, s)
+                                  : launch_attn_typed<float>(a, pv, blocks_per_page, c, geom->head_dim, s);
+}
+
+}  // extern "C"

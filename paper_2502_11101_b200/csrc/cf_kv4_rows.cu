@@ -1,0 +1,262 @@
+// Rows of keys and values into the 4-bit pool and back (cf_kv4_write, cf_kv4_read).
+//
+// Both stream: 4 bytes in and 1.1 out per pair of numbers, or the reverse, so they are laid out for memory.  Eight lanes have a
+// row of a kv head: lane u holds dims 4u .. 4u+3 of every group of 32, which are the bytes of its own value codes (8 bytes that
+// lie together in the block) and half of a key word, so that one exchange with its neighbour gives each of the two 8 bytes
+// of key codes to store.  A warp has four rows: together they write whole 32-byte sectors of value codes.
+#include "cf_kv4.cuh"
+
+namespace cf {
+
+using namespace kv4;
+
+namespace {
+
+constexpr int kRowThreads = 256;
+constexpr int kRowsPerWarp = 4;
+
+// Four consecutive numbers as fp32.
+template <typename T> __device__ __forceinline__ void load4(const T* p, float (&x)[4]);
+template <> __device__ __forceinline__ void load4<float>(const float* p, float (&x)[4]) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+}
+template <> __device__ __forceinline__ void load4<__nv_bfloat16>(const __nv_bfloat16* p, float (&x)[4]) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    x[0] = bf16_low(v.x), x[1] = bf16_high(v.x), x[2] = bf16_low(v.y), x[3] = bf16_high(v.y);
+}
+template <typename T> __device__ __forceinline__ void store4(T* p, const float (&x)[4]);
+template <> __device__ __forceinline__ void store4<float>(float* p, const float (&x)[4]) {
+    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+}
+template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, const float (&x)[4]) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+
+// The scale of a group whose largest magnitude has these bits: bf16 bits, and whether codes other than 0 are kept.
+__device__ __forceinline__ uint32_t scale_of(uint32_t amax, float& scale) {
+    scale = 0.f;
+    if (amax >= 0x7f800000u) return 0x7fffu;                       // not finite
+    // one rounding: a quotient by 6 of 24 bits that is not a tie between bf16 numbers is no nearer to one than its rounding
+    const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__uint_as_float(amax), 6.f)));
+    if (s < 1.1754944e-38f) return 0u;
+    scale = s;
+    return __float_as_uint(s) >> 16;
+}
+
+// Codes of a lane's four numbers of a group, 16 bits.
+__device__ __forceinline__ uint32_t codes4(const float (&x)[4], float scale) {
+    if (scale == 0.f) return 0u;
+    return two_codes(__fdiv_rn(x[0], scale), __fdiv_rn(x[1], scale)) | two_codes(__fdiv_rn(x[2], scale), __fdiv_rn(x[3], scale)) << 8;
+}
+
+// A lane's dims of one row (of keys or values): codes of group j in 16 bits of `codes`, all groups' scales in `scales`.
+template <typename T, int D>
+__device__ __forceinline__ void quantise(const T* row, int u, uint32_t (&codes)[D / 64], uint32_t (&scales)[D / 64]) {
+    float x[D / 32][4];
+    uint32_t amax[D / 32];
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) load4<T>(row + 32 * j + 4 * u, x[j]);
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+        uint32_t a = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a = max(a, __float_as_uint(x[j][i]) & 0x7fffffffu);     // magnitudes order as integers, NaN on top
+        amax[j] = a;
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1)
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) amax[j] = max(amax[j], __shfl_xor_sync(0xffffffffu, amax[j], o));
+#pragma unroll
+    for (int j = 0; j < D / 32; j += 2) {
+        float s0, s1;
+        scales[j / 2] = scale_of(amax[j], s0);
+        scales[j / 2] |= scale_of(amax[j + 1], s1) << 16;
+        codes[j / 2] = codes4(x[j], s0) | codes4(x[j + 1], s1) << 16;
+    }
+}
+
+template <int N> struct Words;
+template <> struct Words<1> { using type = uint32_t; };
+template <> struct Words<2> { using type = uint2; };
+template <int N> __device__ __forceinline__ void store_words(unsigned char* p, const uint32_t (&w)[N]) {
+    if (N == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[N - 1]);
+    else *reinterpret_cast<uint32_t*>(p) = w[0];
+}
+template <int N> __device__ __forceinline__ void load_words(const unsigned char* p, uint32_t (&w)[N]) {
+    if (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        w[0] = v.x, w[N - 1] = v.y;
+    } else {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+}
+
+// Words of key codes from a lane's codes and back.  Lane u holds half u & 1 of the words of every group; it stores the
+// words of groups (u & 1) * D/64 and up, D/64 of them, which lie together.
+template <int D> __device__ __forceinline__ void to_key_words(int u, const uint32_t (&codes)[D / 64], uint32_t (&words)[D / 64]) {
+    if (D == 128) {
+        const uint32_t theirs = __shfl_xor_sync(0xffffffffu, u & 1 ? codes[0] : codes[D / 64 - 1], 1);
+        const uint32_t mine = u & 1 ? codes[D / 64 - 1] : codes[0];
+        const uint32_t lo = u & 1 ? theirs : mine, hi = u & 1 ? mine : theirs;      // of dims 8t .. 8t+3 and 8t+4 .. 8t+7
+        words[0] = __byte_perm(lo, hi, 0x5410);
+        words[D / 64 - 1] = __byte_perm(lo, hi, 0x7632);
+    } else {
+        const uint32_t theirs = __shfl_xor_sync(0xffffffffu, codes[0], 1);
+        words[0] = u & 1 ? __byte_perm(theirs, codes[0], 0x7632) : __byte_perm(codes[0], theirs, 0x5410);
+    }
+}
+template <int D> __device__ __forceinline__ void from_key_words(int u, const uint32_t (&words)[D / 64], uint32_t (&codes)[D / 64]) {
+    if (D == 128) {
+        const uint32_t lo = __byte_perm(words[0], words[D / 64 - 1], 0x5410), hi = __byte_perm(words[0], words[D / 64 - 1], 0x7632);
+        const uint32_t theirs = __shfl_xor_sync(0xffffffffu, u & 1 ? lo : hi, 1);
+        codes[0] = u & 1 ? theirs : lo;
+        codes[D / 64 - 1] = u & 1 ? hi : theirs;
+    } else {
+        const uint32_t theirs = __shfl_xor_sync(0xffffffffu, words[0], 1);
+        codes[0] = u & 1 ? __byte_perm(theirs, words[0], 0x7632) : __byte_perm(words[0], theirs, 0x5410);
+    }
+}
+
+template <typename T, int D>
+__device__ __forceinline__ void dequantise(const uint32_t (&codes)[D / 64], const uint32_t (&scales)[D / 64], int u, T* row) {
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+        const uint32_t w = codes[j / 2];
+        const uint32_t a = j & 1 ? two_numbers<2>(w) : two_numbers<0>(w), b = j & 1 ? two_numbers<3>(w) : two_numbers<1>(w);
+        const float s = j & 1 ? bf16_high(scales[j / 2]) : bf16_low(scales[j / 2]);
+        const float2 fa = __half22float2(*reinterpret_cast<const __half2*>(&a)), fb = __half22float2(*reinterpret_cast<const __half2*>(&b));
+        const float x[4] = {fa.x * s, fa.y * s, fb.x * s, fb.y * s};
+        store4<T>(row + 32 * j + 4 * u, x);
+    }
+}
+
+struct RowArgs {
+    int n_rows, n_kv_heads, page_rows, n_layers;
+    long long n_slots, kv_layer_stride, row_stride, kv4_layer_stride;
+    const long long* slots;
+    int* status;
+};
+
+// Where a slot's row lies: the block, and the row in it; false for a row that goes nowhere.
+__device__ __forceinline__ bool find_row(const RowArgs& a, Divisor page_rows, int row, int head, int block_size, size_t& at, int& r, bool report) {
+    const long long slot = row < a.n_rows ? a.slots[row] : -1;
+    if (slot < 0) return false;
+    if (slot >= a.n_slots) {
+        if (report) atomicCAS(a.status, 0, CF_ERR_RANGE);
+        return false;
+    }
+    const long long page = slot < 0x7fffffffLL - a.page_rows ? page_rows.quotient((int)slot) : slot / a.page_rows;
+    const int in_page = (int)(slot - page * a.page_rows);
+    at = ((size_t)(page * a.n_kv_heads + head) * (a.page_rows / kBlockRows) + in_page / kBlockRows) * block_size;
+    r = in_page % kBlockRows;
+    return true;
+}
+
+// WRITE: rows to slots; otherwise slots to rows.
+template <typename T, int D, bool WRITE>
+__global__ void __launch_bounds__(kRowThreads)
+rows_kernel(RowArgs a, Divisor page_rows, Divisor heads, Divisor quads, T* k, T* v, unsigned char* kv4) {
+    chain_next();
+    chain_wait();
+    const int lane = threadIdx.x & 31, u = lane & 7;
+    const int item = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);      // (layer, four rows, head)
+    const int rest = heads.quotient(item), head = item - rest * a.n_kv_heads;
+    const int layer = quads.quotient(rest), quad = rest - layer * (int)quads.d;
+    if (layer >= a.n_layers) return;                                            // whole warps
+    const int row = quad * kRowsPerWarp + (lane >> 3);
+    size_t at = 0;
+    int r = 0;
+    const bool valid = find_row(a, page_rows, row, head, block_bytes(D), at, r, layer == 0 && head == 0 && u == 0);
+    if (__all_sync(0xffffffffu, !valid)) return;
+    unsigned char* block = kv4 + (size_t)layer * a.kv4_layer_stride + at;
+    const size_t src = (size_t)layer * a.kv_layer_stride + (size_t)(valid ? row : quad * kRowsPerWarp) * a.row_stride + head * D;
+    uint32_t codes[D / 64], scales[D / 64], words[D / 64];
+    if (WRITE) {
+        quantise<T, D>(k + src, u, codes, scales);
+        to_key_words<D>(u, codes, words);
+        if (valid) {
+            store_words<D / 64>(block + key_code_at<D>(r) + (u >> 1) * (D / 8) + (u & 1) * (D / 16), words);
+            if (u == 0) store_words<D / 64>(block + key_scale_at<D>(r), scales);
+        }
+        quantise<T, D>(v + src, u, codes, scales);
+        if (valid) {
+            store_words<D / 64>(block + value_code_at<D>(r, u), codes);
+            if (u == 0) store_words<D / 64>(block + value_scale_at<D>(r), scales);
+        }
+    } else {
+        load_words<D / 64>(block + key_code_at<D>(r) + (u >> 1) * (D / 8) + (u & 1) * (D / 16), words);
+        load_words<D / 64>(block + key_scale_at<D>(r), scales);
+        from_key_words<D>(u, words, codes);
+        if (valid) dequantise<T, D>(codes, scales, u, k + src);
+        load_words<D / 64>(block + value_code_at<D>(r, u), codes);
+        load_words<D / 64>(block + value_scale_at<D>(r), scales);
+        if (valid) dequantise<T, D>(codes, scales, u, v + src);
+    }
+}
+
+template <typename T, int D, bool WRITE>
+int launch_rows(const RowArgs& a, const void* k, const void* v, const void* kv4, cudaStream_t stream) {
+    const int quads = (a.n_rows + kRowsPerWarp - 1) / kRowsPerWarp;
+    const long long items = (long long)quads * a.n_kv_heads * a.n_layers;
+    if (items > 0x7fffffffLL - 64) return CF_ERR_INVALID_ARG;
+    const unsigned blocks = (unsigned)((items + kRowThreads / 32 - 1) / (kRowThreads / 32));
+    return launch_chained(rows_kernel<T, D, WRITE>, dim3(blocks), kRowThreads, 0, stream, a, Divisor(a.page_rows), Divisor(a.n_kv_heads),
+                          Divisor(quads), static_cast<T*>(const_cast<void*>(k)), static_cast<T*>(const_cast<void*>(v)),
+                          static_cast<unsigned char*>(const_cast<void*>(kv4)));
+}
+
+template <bool WRITE>
+int run_rows(const cf_geom* geom, const cf_pages* pages, int n_layers, int n_rows, const int64_t* slots, const void* k, const void* v,
+             long long kv_layer_stride, long long row_stride, const void* kv4, long long kv4_layer_stride, void* stream) {
+    int rc = validate(geom, nullptr);
+    if (rc == CF_OK) rc = check_pages(pages);
+    if (rc != CF_OK) return rc;
+    if (n_layers <= 0 || n_rows < 0) return CF_ERR_INVALID_ARG;
+    if (n_rows == 0) return CF_OK;
+    if (!slots || !k || !v || !kv4) return CF_ERR_INVALID_ARG;
+    const int esize = geom->dtype == CF_BF16 ? 2 : 4;
+    const long long row_elems = (long long)geom->n_kv_heads * geom->head_dim;
+    for (const void* p : {k, v, kv4})
+        if (reinterpret_cast<uintptr_t>(p) % 16) return CF_ERR_INVALID_ARG;
+    if (row_stride < row_elems || (row_stride * esize) % 16 || (kv_layer_stride * esize) % 16 || kv4_layer_stride % 16)
+        return CF_ERR_INVALID_ARG;
+    if (n_layers > 1 && (kv_layer_stride < (n_rows - 1) * row_stride + row_elems ||
+                         kv4_layer_stride < (long long)cf_kv4_layer_bytes(geom, pages)))
+        return CF_ERR_INVALID_ARG;
+    const RowArgs a = {n_rows, geom->n_kv_heads, pages->page_rows, n_layers, (long long)pages->n_pages * pages->page_rows,
+                       kv_layer_stride, row_stride, kv4_layer_stride, reinterpret_cast<const long long*>(slots), pages->status};
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (geom->dtype == CF_BF16)
+        return geom->head_dim == 128 ? launch_rows<__nv_bfloat16, 128, WRITE>(a, k, v, kv4, s) : launch_rows<__nv_bfloat16, 64, WRITE>(a, k, v, kv4, s);
+    return geom->head_dim == 128 ? launch_rows<float, 128, WRITE>(a, k, v, kv4, s) : launch_rows<float, 64, WRITE>(a, k, v, kv4, s);
+}
+
+}  // namespace
+
+}  // namespace cf
+
+using namespace cf;
+
+extern "C" {
+
+size_t cf_kv4_layer_bytes(const cf_geom* geom, const cf_pages* pages) {
+    if (validate(geom, nullptr) != CF_OK || check_pages(pages) != CF_OK) return 0;
+    return (size_t)pages->n_pages * geom->n_kv_heads * (pages->page_rows / kv4::kBlockRows) * kv4::block_bytes(geom->head_dim);
+}
+
+int cf_kv4_write(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t n_rows, const int64_t* slots,
+                 const void* k, const void* v, int64_t kv_layer_stride, int64_t row_stride, void* kv4,
+                 int64_t kv4_layer_stride, void* stream) {
+    return run_rows<true>(geom, pages, n_layers, n_rows, slots, k, v, kv_layer_stride, row_stride, kv4, kv4_layer_stride, stream);
+}
+
+int cf_kv4_read(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t n_rows, const int64_t* slots,
+                const void* kv4, int64_t kv4_layer_stride, void* k, void* v, int64_t kv_layer_stride, int64_t row_stride,
+                void* stream) {
+    return run_rows<false>(geom, pages, n_layers, n_rows, slots, k, v, kv_layer_stride, row_stride, kv4, kv4_layer_stride, stream);
+}
+
+}  // extern "C"
