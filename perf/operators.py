@@ -403,7 +403,8 @@ def _handle(s, flat):
     import paper_2502_11101_b200 as cf
     case = s["case"]
     table, rows, free, count, status = _views(case, flat, s["n_pages"])
-    made = {"cf": cf, "pages": cf.make_pages(table, rows, free, count, status, case["page_rows"])}
+    made = {"cf": cf, "pages": cf.make_pages(table, rows, free, count, status, case["page_rows"]), "views": (table, rows, free, count),
+            "place": torch.arange(s["n_pages"], device="cuda")}
     if "head_dim" in case:
         made["geom"] = cf.make_geom(case.get("q_heads", case["kv_heads"]), case["kv_heads"], case["head_dim"], _DTYPES[case["dtype"]], 32768, 1.0e6)
     return made
@@ -412,11 +413,11 @@ def _handle(s, flat):
 def _own_pages(s):
     if "handle" not in s:
         s["handle"] = _handle(s, s["work"])
-    cf = s["handle"]["cf"]
+    hd = s["handle"]
     s["work"].copy_(s["init"])
-    cf.cf_pages_resize(s["handle"]["pages"], s["target"], 0, s["slots"])
-    table, rows, free, count, _ = _views(s["case"], s["work"], s["n_pages"])
-    return _pages_answer(s, table, rows, free, count)
+    hd["cf"].cf_pages_resize(hd["pages"], s["target"], 0, s["slots"])
+    table, rows, free, count = hd["views"]
+    return {"table": table, "rows": rows, "count": count, "slots": s["slots"], "free": torch.where(hd["place"] < count, free, -1)}
 
 
 def _own_rows(s):
