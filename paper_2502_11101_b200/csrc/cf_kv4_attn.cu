@@ -38,11 +38,23 @@ namespace {
 
 constexpr int kWarps = 8;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kStages = 4;
+constexpr int kStages = 2;                        // steps of the ring
+constexpr int kStepBlocks = 2;                    // blocks of a step
+constexpr int kStepRows = kStepBlocks * kBlockRows;
 constexpr int kMergeThreads = 256;
 constexpr float kSlack = 8.f;                     // how far a logit may lie above the running maximum (base 2)
 constexpr int kHead = 7;                          // P is at most 2^kSlack * 2^kHead, below fp16's 2^16
 constexpr int kLeastExponent = -110;
+constexpr int kMostCost = 32;                     // of a unit, in steps
+#ifndef FACTOR
+#define FACTOR 2.0
+#define LEAST1 4
+#define COST1 3
+#endif
+#ifndef LEAST
+#define LEAST kWarps
+#define COST 16
+#endif
 
 struct Kv4Args {
     const void* q;
@@ -53,8 +65,9 @@ struct Kv4Args {
     float* part_ml;                               // [2 shares][2][columns]
     int4* marks;                                  // [shares] what a share leaves for the merge: parts, layer, request, head * tiles + tile
     long long q_layer_stride, kv4_layer_stride, out_layer_stride;
-    int n_layers, q_len, n_q_heads, n_kv_heads, group, columns, tiles;     // columns = group * q_len of a kv head
-    int n_shares, warps_per_share;
+    int n_layers, q_len, n_q_heads, n_kv_heads, columns;                   // columns = query heads of a kv head * q_len
+    Divisor group, tiles, blocks_per_page;
+    int n_shares, warps_per_share, unit_cost;
     long long least_share;
     float scale_log2;
 };
@@ -68,6 +81,11 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {
     uint32_t y;
@@ -96,35 +114,41 @@ template <int N> __device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N
     if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
 }
 
-__device__ __forceinline__ int steps_of(int rows) { return max(1, (rows + kBlockRows - 1) / kBlockRows); }
+__device__ __forceinline__ int steps_of(int rows) { return max(1, (rows + kStepRows - 1) / kStepRows); }
 
-// A place on the line: a unit and a block of it.
-struct Place {
+// A share's way along the line.  A unit is as long as its steps and what a unit costs besides, `cost` of them, which come first: so
+// that shares over many short units are not the last to end.
+struct Walk {
     int layer, request, unit;                     // unit = kv head * tiles + tile, within (layer, request)
-    int rows, steps;                              // of the request
-    int step;
+    int rows, length;                             // rows of the request, length of the unit
+    int at;                                       // place in the unit
+    long long left;                               // of the share, from there on
+    __device__ __forceinline__ int end() const { return (int)min((long long)length, at + left); }
+    __device__ __forceinline__ int first_step(int cost) const { return max(0, at - cost); }
+    __device__ __forceinline__ int last_step(int cost) const { return max(0, end() - cost); }
 };
 
-// Steps of all requests, and the place `at` steps along the line (units of a request are neighbours, layers outermost).
 struct Line {
     const PagesView& pv;
-    int units;                                    // per (layer, request)
+    int units, cost;                              // units per (layer, request)
     int most;                                     // rows the table has room for
     __device__ __forceinline__ int rows_of(int b) const { return min(max(pv.rows[b], 0), most); }
-    __device__ __forceinline__ long long steps_of_layer() const {
+    __device__ __forceinline__ long long length_of_layer() const {
         long long sum = 0;
-        for (int b = threadIdx.x & 31; b < pv.n_requests; b += 32) sum += steps_of(rows_of(b));
+#pragma unroll 4
+        for (int b = threadIdx.x & 31; b < pv.n_requests; b += 32) sum += steps_of(rows_of(b)) + cost;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         return sum * units;
     }
-    __device__ __forceinline__ Place find(long long at, long long per_layer) const {
+    __device__ __forceinline__ Walk find(long long at, long long left, long long per_layer) const {
         const int lane = threadIdx.x & 31;
-        Place p = {};
+        Walk p = {};
+        p.left = left;
         if (at >= per_layer) p.layer = (int)(at / per_layer), at -= p.layer * per_layer;
         for (int b0 = 0;; b0 += 32) {
-            const int b = b0 + lane, rows = b < pv.n_requests ? rows_of(b) : 0, steps = b < pv.n_requests ? steps_of(rows) : 0;
-            long long end = (long long)steps * units;
+            const int b = b0 + lane, rows = b < pv.n_requests ? rows_of(b) : 0, length = b < pv.n_requests ? steps_of(rows) + cost : 0;
+            long long end = (long long)length * units;
             const long long mine = end;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -136,94 +160,101 @@ struct Line {
                 const int src = behind != 0 ? __ffs(behind) - 1 : 0;
                 p.request = b0 + src;
                 p.rows = __shfl_sync(0xffffffffu, rows, src);
-                p.steps = __shfl_sync(0xffffffffu, steps, src);
-                const int within = (int)(at - __shfl_sync(0xffffffffu, end - mine, src));    // units * steps: below 2^31 for every cache that fits
-                p.unit = within / p.steps;
-                p.step = within - p.unit * p.steps;
+                p.length = __shfl_sync(0xffffffffu, length, src);
+                const int within = (int)(at - __shfl_sync(0xffffffffu, end - mine, src));    // the host has seen to 32 bits
+                p.unit = within / p.length;
+                p.at = within - p.unit * p.length;
                 return p;
             }
             at -= __shfl_sync(0xffffffffu, end, 31);
         }
     }
-    __device__ __forceinline__ void next_unit(Place& p) const {
-        p.step = 0;
-        if (++p.unit < units) return;
+    // To the beginning of the next unit; there is one where something is left.
+    __device__ __forceinline__ void next_unit(Walk& p) const {
+        p.left -= p.end() - p.at;
+        p.at = 0;
+        if (p.left <= 0 || ++p.unit < units) return;
         p.unit = 0;
         if (++p.request == pv.n_requests) p.request = 0, ++p.layer;
         p.rows = rows_of(p.request);
-        p.steps = steps_of(p.rows);
+        p.length = steps_of(p.rows) + cost;
     }
 };
 
-// The copies of a warp's blocks: it takes every stride-th block from `first` on of each unit of its share.
+// The copies of a warp's steps: it takes every stride-th step from `first` on of each unit of its share.  The walk lies in shared
+// memory: it is looked at once in sixteen steps.
 template <int D>
 struct Feeder {
     static constexpr int kBytes = block_bytes(D);
     const PagesView& pv;
     const Kv4Args& a;
     const Line& line;
-    Divisor blocks_per_page;
-    Place p;
-    long long left;                               // steps of the share from the beginning of p's unit (from p.step) on
+    Walk* walk;
+    int* next;                                    // the unit's next step to look up
     int first, stride;
-    int ready, used;                              // blocks whose addresses the lanes hold; blocks of them that were issued
-    const unsigned char* address;                 // lane l's block
-    int base;                                     // next step of the unit to look up
+    int ready, used;                              // steps whose addresses the lanes hold, two lanes a step; how many of them were issued
+    const unsigned char* address;                 // lane l's block, nullptr for a block behind the rows
     uint32_t ring, bars;
-    int stage;
     unsigned issued;
+    bool ended;
 
-    // The next up to 32 blocks: every lane looks one up.
     __device__ __forceinline__ void look_up() {
         const int lane = threadIdx.x & 31;
-        while (true) {
-            const int end = (int)min((long long)p.steps, p.step + left);
-            const int n = base < end ? (end - base + stride - 1) / stride : 0;
+        __syncwarp();
+        Walk p = *walk;
+        int step = *next;
+        __syncwarp();
+        ready = used = 0;
+        while (p.left > 0) {
+            const int last = p.last_step(line.cost);
+            const int n = step < last ? (last - step + stride - 1) / stride : 0;
             if (n > 0) {
-                ready = min(32, n);
-                used = 0;
+                ready = min(16, n);
                 address = nullptr;
-                if (lane < ready) {
-                    const int step = base + lane * stride;
-                    const int column = blocks_per_page.quotient(step);
+                const int block = kStepBlocks * (step + (lane >> 1) * stride) + (lane & 1);
+                if ((lane >> 1) < ready && (block == 0 || block * kBlockRows < p.rows)) {
+                    const int column = a.blocks_per_page.quotient(block);
                     int page = pv.table[(size_t)p.request * pv.table_cols + column];
                     if ((unsigned)page >= (unsigned)pv.n_pages) {
                         if (p.rows > 0) atomicCAS(pv.status, 0, CF_ERR_RANGE);   // a request without rows has no pages
                         page = 0;
                     }
-                    const int head = p.unit / a.tiles;
+                    const int head = a.tiles.quotient(p.unit);
                     address = a.kv4 + (size_t)p.layer * a.kv4_layer_stride +
-                              (((size_t)page * a.n_kv_heads + head) * blocks_per_page.d + (step - column * (int)blocks_per_page.d)) * kBytes;
+                              (((size_t)page * a.n_kv_heads + head) * a.blocks_per_page.d + (block - column * (int)a.blocks_per_page.d)) * kBytes;
                 }
-                base += ready * stride;
-                return;
-            }
-            left -= end - p.step;
-            if (left <= 0) {
-                ready = used = 0;
-                return;
+                step += ready * stride;
+                break;
             }
             line.next_unit(p);
-            base = first;
+            step = first;
         }
+        if (lane == 0) *walk = p, *next = step;
+        __syncwarp();
     }
-    // Issues the next block's copy into the stage that was read last.
+    // Issues the next step's copies into the stage that was read last.
     __device__ __forceinline__ void feed() {
         if (used == ready) {
-            if (ready == 0) return;
+            if (ended) return;
             look_up();
-            if (ready == 0) return;
+            ended = ready == 0;
+            if (ended) return;
         }
-        if ((int)(threadIdx.x & 31) == used) {
+        const int lane = threadIdx.x & 31;
+        const uint32_t stage = issued % kStages;
+        if ((lane >> 1) == used) {
             const uint32_t bar = bars + 8 * stage;
-            mbar_expect_tx(bar, kBytes);
-            asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ring + stage * kBytes),
-                         "l"(address), "r"(kBytes), "r"(bar)
-                         : "memory");
+            if (address) {
+                mbar_expect_tx(bar, kBytes);
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ring + (stage * kStepBlocks + (lane & 1)) * kBytes),
+                             "l"(address), "r"(kBytes), "r"(bar)
+                             : "memory");
+            } else {
+                tc::mbar_arrive(bar);
+            }
         }
         ++used;
         ++issued;
-        stage = stage + 1 == kStages ? 0 : stage + 1;
     }
 };
 
@@ -244,33 +275,36 @@ __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, float a,
 // Results of a column: where they go, by the column's number within the kv head (token-major).
 template <typename T, int D>
 __device__ __forceinline__ T* out_row(const Kv4Args& a, int n_requests, int layer, int request, int head, int column) {
-    const int token = column / a.group, h = head * a.group + column % a.group;
+    const int token = a.group.quotient(column), h = head * (int)a.group.d + a.group.remainder(column);
     return static_cast<T*>(a.out) + (size_t)layer * a.out_layer_stride + (((size_t)request * a.q_len + token) * a.n_q_heads + h) * D;
 }
 __device__ __forceinline__ void store_lse(const Kv4Args& a, int n_requests, int layer, int request, int head, int column, float m, float l) {
     if (!a.lse) return;
-    const int token = column / a.group, h = head * a.group + column % a.group;
+    const int token = a.group.quotient(column), h = head * (int)a.group.d + a.group.remainder(column);
     a.lse[(((size_t)layer * n_requests + request) * a.n_q_heads + h) * a.q_len + token] = l > 0.f || l != l ? m * kLn2 + logf(l) : -INFINITY;
 }
 
 template <typename T, int D, int NT>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
-kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
+kv4_attn_kernel(Kv4Args args, PagesView pv) {
     chain_next();
     constexpr int kBytes = block_bytes(D);
+    constexpr int kRing = kStages * kStepBlocks * kBytes;    // of a warp
     constexpr int kGroups = D / 32;
     constexpr int kCols = 8 * NT;
     constexpr int kParts = IsF32<T>::value ? 2 : 1;          // fp16 numbers per query or probability
     constexpr int kOStride = D + 4;                          // floats between columns in shared memory: no bank conflicts
     extern __shared__ __align__(128) unsigned char smem[];
-    unsigned char* s_ring = smem;                            // [kWarps][kStages][kBytes]
-    float* s_o = reinterpret_cast<float*>(smem + kWarps * kStages * kBytes);    // [kWarps][kCols][kOStride]
+    unsigned char* s_ring = smem;                            // [kWarps][kRing]
+    float* s_o = reinterpret_cast<float*>(smem + kWarps * kRing);               // [kWarps][kCols][kOStride]
     float* s_m = s_o + kWarps * kCols * kOStride;            // [kWarps][kCols]
     float* s_l = s_m + kWarps * kCols;                       // [kWarps][kCols]
     unsigned long long* s_bars = reinterpret_cast<unsigned long long*>(s_l + kWarps * kCols);   // [kWarps][kStages]
+    __shared__ Walk s_walk[kWarps];
+    __shared__ int s_next[kWarps];
     __shared__ volatile int s_abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    if (lane < kStages) mbar_init(smem_u32(s_bars + warp * kStages + lane), 1);
+    if (lane < kStages) mbar_init(smem_u32(s_bars + warp * kStages + lane), kStepBlocks);
     if (tid == 0) s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
@@ -280,32 +314,31 @@ kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
 
     const bool together = a.warps_per_share > 1;             // the CTA's warps share a share
     const int share = together ? (int)blockIdx.x : (int)blockIdx.x * kWarps + warp;
-    const Line line = {pv, a.n_kv_heads * a.tiles, pv.table_cols * pv.page_rows};
-    const long long per_layer = line.steps_of_layer(), total = per_layer * a.n_layers;
+    const int cost = a.unit_cost;
+    const Line line = {pv, a.n_kv_heads * (int)a.tiles.d, cost, pv.table_cols * pv.page_rows};
+    const long long per_layer = line.length_of_layer(), total = per_layer * a.n_layers;
     const long long size = max(a.least_share, (total + a.n_shares - 1) / a.n_shares);
-    const long long begin = share * size;
-    long long left = min(size, total - begin);
+    const long long begin = share * size, mine = min(size, total - begin);
     if (lane == 0 && (!together || warp == 0)) a.marks[share] = make_int4(0, 0, 0, 0);
     if (share == 0 && (!together || warp == 0))
         for (int b = lane; b < pv.n_requests; b += 32)
             if (pv.rows[b] < 0 || pv.rows[b] > line.most) atomicCAS(pv.status, 0, CF_ERR_RANGE);
-    if (left <= 0) return;                                   // a warp's or the whole CTA's, no barrier follows
+    if (mine <= 0) return;                                   // a warp's or the whole CTA's, no barrier follows
 
-    Place p = line.find(begin, per_layer);
+    Walk p = line.find(begin, mine, per_layer);
     const int first_step = together ? warp : 0, stride = together ? kWarps : 1;
-    const uint32_t ring = smem_u32(s_ring) + warp * kStages * kBytes, bars = smem_u32(s_bars + warp * kStages);
-    Feeder<D> feeder = {pv, a, line, blocks_per_page, p, left, first_step, stride, 0, 0, nullptr, p.step + first_step, ring, bars, 0, 0u};
-    feeder.look_up();
-#pragma unroll
+    const uint32_t ring = smem_u32(s_ring) + warp * kRing, bars = smem_u32(s_bars + warp * kStages);
+    if (lane == 0) s_walk[warp] = p, s_next[warp] = p.first_step(cost) + first_step;
+    Feeder<D> feeder = {pv, a, line, s_walk + warp, s_next + warp, first_step, stride, 0, 0, nullptr, ring, bars, 0u, false};
+#pragma unroll 1
     for (int i = 0; i < kStages; ++i) feeder.feed();
-    int stage = 0, phase = 0;
-    unsigned taken = 0;                                      // copies that were waited for
+    unsigned taken = 0;                                      // steps that were waited for
     bool given_up = false;
-    bool whole_start = p.step == 0;                          // the share's part of the unit begins with the unit
 
-    while (left > 0) {                                       // a unit, or the share's part of one
-        const int end = (int)min((long long)p.steps, p.step + left);
-        const int head = p.unit / a.tiles, col0 = (p.unit - head * a.tiles) * kCols;
+    for (; p.left > 0; line.next_unit(p)) {                  // a unit, or the share's part of one
+        const int start = p.first_step(cost), last = p.last_step(cost);
+        if (last <= start) continue;                         // the unit's first step is the next share's
+        const int head = a.tiles.quotient(p.unit), col0 = (p.unit - head * (int)a.tiles.d) * kCols;
         // the queries: lane (g, t) holds dims 32 j + 8 t .. + 7 of column g of every tile of eight
         uint32_t qf[NT][kParts][kGroups][2][2];
         float cs[NT][2];                                     // what turns sums of codes into base-2 logits, columns 2t and 2t + 1
@@ -316,7 +349,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
             float x[kGroups][8];
             uint32_t amax = 0;
             if (column < a.columns) {
-                const int token = column / a.group, h = head * a.group + column % a.group;
+                const int token = a.group.quotient(column), h = head * (int)a.group.d + a.group.remainder(column);
                 const T* q = static_cast<const T*>(a.q) + (size_t)p.layer * a.q_layer_stride + (((size_t)p.request * a.q_len + token) * a.n_q_heads + h) * D + 8 * t;
 #pragma unroll
                 for (int j = 0; j < kGroups; ++j) {
@@ -352,12 +385,13 @@ kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
             for (int i = 0; i < 2; ++i) {
                 cs[n][i] = a.scale_log2 * __shfl_sync(0xffffffffu, up, (2 * t + i) * 4);
                 const int mine = col0 + 8 * n + 2 * t + i;
-                sees[n][i] = mine < a.columns ? p.rows - a.q_len + 1 + mine / a.group : p.rows;
+                sees[n][i] = mine < a.columns ? p.rows - a.q_len + 1 + a.group.quotient(mine) : p.rows;
             }
         }
-        const int all_see = p.rows - a.q_len + 1 + col0 / a.group;       // what the tile's first column sees, the fewest
+        const int all_see = p.rows - a.q_len + 1 + a.group.quotient(col0);       // what the tile's first column sees, the fewest
 
-        float o[NT][kGroups][2][4], m[NT][2], l[NT][2];
+        // base: what logits are taken from (the running maximum, 0 before there is one); slack: how far above it they may lie
+        float o[NT][kGroups][2][4], base[NT][2], slack[NT][2], l[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -366,23 +400,23 @@ kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) o[n][j][i][k] = 0.f;
-            m[n][0] = m[n][1] = -INFINITY;
+            base[n][0] = base[n][1] = 0.f;
+            slack[n][0] = slack[n][1] = -INFINITY;
             l[n][0] = l[n][1] = 0.f;
         }
         int exponent = kLeastExponent;                       // values are taken in units of 2^(exponent - kHead)
-        float scale_limit = __int_as_float((127 + exponent) << 23), scale_down = exp2f((float)(kHead - exponent));
+        uint32_t scale_limit = (uint32_t)(127 + exponent) * 0x00800080u;   // 2^exponent as bf16, twice
+        float scale_down = exp2f((float)(kHead - exponent));
 
-        for (int step = p.step + first_step; step < end; step += stride) {
-            const uint32_t block = ring + stage * kBytes;
-            if (!given_up && !tc::mbar_wait(bars + 8 * stage, phase, &s_abort)) given_up = true;
+        for (int step = start + first_step; step < last; step += stride) {
+            const uint32_t stage = taken % kStages, blocks = ring + stage * kStepBlocks * kBytes;
+            if (!given_up && !tc::mbar_wait(bars + 8 * stage, taken / kStages & 1, &s_abort)) given_up = true;
             if (!given_up) ++taken;
-            // S^T of 16 keys
-            float s[NT][4];
+            // S^T of 32 keys
+            float s[kStepBlocks][NT][4];
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
-            {
+            for (int x = 0; x < kStepBlocks; ++x) {
+                const uint32_t block = blocks + x * kBytes;
                 uint32_t k0[kGroups], k1[kGroups], ks0[kGroups / 2], ks1[kGroups / 2];
                 lds<kGroups>(block + key_code_at<D>(g) + t * (D / 8), k0);
                 lds<kGroups>(block + key_code_at<D>(g + 8) + t * (D / 8), k1);
@@ -395,102 +429,128 @@ kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
                     const float f0 = j & 1 ? bf16_high(ks0[j / 2]) : bf16_low(ks0[j / 2]), f1 = j & 1 ? bf16_high(ks1[j / 2]) : bf16_low(ks1[j / 2]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        float c[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int i = 0; i < kParts; ++i) {
-                            mma_f16(c, a00, a10, a20, a30, qf[n][i][j][0][0], qf[n][i][j][0][1]);
-                            mma_f16(c, a01, a11, a21, a31, qf[n][i][j][1][0], qf[n][i][j][1][1]);
+                        float c[4];
+                        mma_f16_first(c, a00, a10, a20, a30, qf[n][0][j][0][0], qf[n][0][j][0][1]);
+                        mma_f16(c, a01, a11, a21, a31, qf[n][0][j][1][0], qf[n][0][j][1][1]);
+                        if (kParts == 2) {
+                            mma_f16(c, a00, a10, a20, a30, qf[n][kParts - 1][j][0][0], qf[n][kParts - 1][j][0][1]);
+                            mma_f16(c, a01, a11, a21, a31, qf[n][kParts - 1][j][1][0], qf[n][kParts - 1][j][1][1]);
                         }
-                        s[n][0] = fmaf(c[0], f0, s[n][0]), s[n][1] = fmaf(c[1], f0, s[n][1]);
-                        s[n][2] = fmaf(c[2], f1, s[n][2]), s[n][3] = fmaf(c[3], f1, s[n][3]);
+                        if (j == 0) {
+                            s[x][n][0] = c[0] * f0, s[x][n][1] = c[1] * f0, s[x][n][2] = c[2] * f1, s[x][n][3] = c[3] * f1;
+                        } else {
+                            s[x][n][0] = fmaf(c[0], f0, s[x][n][0]), s[x][n][1] = fmaf(c[1], f0, s[x][n][1]);
+                            s[x][n][2] = fmaf(c[2], f1, s[x][n][2]), s[x][n][3] = fmaf(c[3], f1, s[x][n][3]);
+                        }
                     }
                 }
             }
-            uint32_t vw[2][2][kGroups / 2];                  // [half][odd][groups two by two]
-            float vs[2][kGroups];                            // scales of keys g and g + 8
-            {
-                uint32_t w[kGroups], ws[kGroups / 2];
+            uint32_t ws[kStepBlocks][2][kGroups / 2];        // scales of keys g and g + 8
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    lds<kGroups>(block + value_code_at<D>(8 * h + 2 * t, g), w);
+            for (int x = 0; x < kStepBlocks; ++x)
 #pragma unroll
-                    for (int i = 0; i < kGroups / 2; ++i) vw[h][0][i] = w[i], vw[h][1][i] = w[kGroups / 2 + i];
-                    lds<kGroups / 2>(block + value_scale_at<D>(g + 8 * h), ws);
-#pragma unroll
-                    for (int i = 0; i < kGroups / 2; ++i) vs[h][2 * i] = bf16_low(ws[i]), vs[h][2 * i + 1] = bf16_high(ws[i]);
-                }
-            }
-            __syncwarp();                                    // the stage has been read
-            if (!given_up) feeder.feed();
-            if (++stage == kStages) stage = 0, phase ^= 1;
+                for (int h = 0; h < 2; ++h) lds<kGroups / 2>(blocks + x * kBytes + value_scale_at<D>(g + 8 * h), ws[x][h]);
 
-            const bool masked = (step + 1) * kBlockRows > all_see;
-            bool raise = false;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int x = 0; x < kStepBlocks; ++x)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[n][i] *= cs[n][i & 1];
-                    if (masked && step * kBlockRows + g + 8 * (i >> 1) >= sees[n][i & 1]) s[n][i] = -INFINITY;
-                    raise |= s[n][i] > m[n][i & 1] + kSlack;
-                }
-            if (masked) {                                    // rows behind the last may hold anything
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[x][n][i] = fmaf(s[x][n][i], cs[n][i & 1], -base[n][i & 1]);
+            if ((step + 1) * kStepRows > all_see) {          // some query does not see some of the keys
                 bool nan = false;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int x = 0; x < kStepBlocks; ++x)
 #pragma unroll
-                    for (int j = 0; j < kGroups; ++j) {
-                        if (step * kBlockRows + g + 8 * h >= p.rows) vs[h][j] = 0.f;
-                        nan |= vs[h][j] != vs[h][j];
+                    for (int h = 0; h < 2; ++h) {
+                        const int row = step * kStepRows + x * kBlockRows + g + 8 * h;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                if (row >= sees[n][i]) s[x][n][2 * h + i] = -INFINITY;
+#pragma unroll
+                        for (int i = 0; i < kGroups / 2; ++i) {
+                            if (row >= p.rows) ws[x][h][i] = 0u;     // rows behind the last may hold anything
+                            nan |= bf16_low(ws[x][h][i]) != bf16_low(ws[x][h][i]) || bf16_high(ws[x][h][i]) != bf16_high(ws[x][h][i]);
+                        }
                     }
-                if (__any_sync(0xffffffffu, nan)) {          // reaches the queries that see the row, and no others
+                if (__any_sync(0xffffffffu, nan)) {          // a NaN reaches the queries that see its row, and no others
 #pragma unroll
                     for (int j = 0; j < kGroups; ++j) {
+                        bool is_nan[kStepBlocks][2];
+#pragma unroll
+                        for (int x = 0; x < kStepBlocks; ++x)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const float y = j & 1 ? bf16_high(ws[x][h][j / 2]) : bf16_low(ws[x][h][j / 2]);
+                                is_nan[x][h] = y != y;
+                                if (is_nan[x][h]) ws[x][h][j / 2] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
+                            }
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
                                 bool hit = false;
 #pragma unroll
-                                for (int h = 0; h < 2; ++h) hit |= vs[h][j] != vs[h][j] && step * kBlockRows + g + 8 * h < sees[n][i];
+                                for (int x = 0; x < kStepBlocks; ++x)
+#pragma unroll
+                                    for (int h = 0; h < 2; ++h) hit |= is_nan[x][h] && step * kStepRows + x * kBlockRows + g + 8 * h < sees[n][i];
                                 // lanes of the same columns: bits t, t + 4, ...
                                 if (__ballot_sync(0xffffffffu, hit) & (0x11111111u << t))
 #pragma unroll
                                     for (int k = 0; k < 2; ++k) o[n][j][k][i] = o[n][j][k][i + 2] = __int_as_float(0x7fffffff);
                             }
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            if (vs[h][j] != vs[h][j]) vs[h][j] = 0.f;
                     }
                 }
             }
-            float vmax = 0.f;
+            bool raise = false;
+            uint32_t most = scale_limit;                     // scales order as integers
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int x = 0; x < kStepBlocks; ++x) {
 #pragma unroll
-                for (int j = 0; j < kGroups; ++j) vmax = fmaxf(vmax, vs[h][j]);
-            raise |= vmax > scale_limit;
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) raise |= s[x][n][i] > slack[n][i & 1];
+#pragma unroll
+                for (int i = 0; i < kGroups / 2; ++i) most = __vmaxu2(most, __vmaxu2(ws[x][0][i], ws[x][1][i]));
+            }
+            raise |= most != scale_limit;
             if (__any_sync(0xffffffffu, raise)) {
+                float vmax = 0.f;
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, x));
+                for (int x = 0; x < kStepBlocks; ++x)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < kGroups / 2; ++i) vmax = fmaxf(vmax, fmaxf(bf16_low(ws[x][h][i]), bf16_high(ws[x][h][i])));
+#pragma unroll
+                for (int y = 4; y < 32; y <<= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, y));
                 float f = 1.f;
-                if (vmax > scale_limit) {
+                if (vmax > bf16_low(scale_limit)) {
                     const int e = min((int)(__float_as_uint(vmax) >> 23) - 126, 127);
                     f = exp2f((float)(exponent - e));
                     exponent = e;
-                    scale_limit = __int_as_float((127 + e) << 23);
+                    scale_limit = (uint32_t)(127 + e) * 0x00800080u;
                     scale_down = exp2f((float)(kHead - e));
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float x = fmaxf(s[n][i], s[n][i + 2]);
+                        float y = -INFINITY;                 // above `base`
 #pragma unroll
-                        for (int y = 4; y < 32; y <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, y));
-                        x = fmaxf(x, m[n][i]);
-                        const float r = x == m[n][i] ? 1.f : exp2_fast(m[n][i] - x);
-                        m[n][i] = x;
+                        for (int x = 0; x < kStepBlocks; ++x) y = fmaxf(y, fmaxf(s[x][n][i], s[x][n][i + 2]));
+#pragma unroll
+                        for (int k = 4; k < 32; k <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, k));
+                        float r = 1.f;
+                        if (slack[n][i] != -INFINITY) y = fmaxf(y, 0.f), r = exp2_fast(-y);
+                        if (y != -INFINITY) {                // otherwise the column has seen nothing yet
+                            base[n][i] += y;
+                            slack[n][i] = kSlack;
+#pragma unroll
+                            for (int x = 0; x < kStepBlocks; ++x) s[x][n][i] -= y, s[x][n][i + 2] -= y;
+                        }
                         l[n][i] *= r;
 #pragma unroll
                         for (int j = 0; j < kGroups; ++j)
@@ -500,47 +560,57 @@ kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
             }
             // the probabilities
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int x = 0; x < kStepBlocks; ++x)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float x = exp2_fast(s[n][i] - m[n][i & 1]);
-                    if (masked && s[n][i] == -INFINITY) x = 0.f;
-                    l[n][i & 1] += x;
-                    s[n][i] = x * scale_down;
-                }
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float y = exp2_fast(s[x][n][i]);
+                        l[n][i & 1] += y;
+                        s[x][n][i] = y * scale_down;
+                    }
             // O^T += V^T P^T, group by group
 #pragma unroll
-            for (int j = 0; j < kGroups; ++j) {
-                constexpr uint32_t kLow = 0x0f0f0f0fu;
-                uint32_t even[2], odd[2];                    // [half]: codes of an even dim of two keys to a byte; of an odd dim
+            for (int x = 0; x < kStepBlocks; ++x) {
+                uint32_t vw[2][kGroups];                     // [half]: groups two by two of an even key's codes, of an odd one's
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t w0 = vw[h][0][j / 2], w1 = vw[h][1][j / 2];
-                    even[h] = (w0 & kLow) | ((w1 << 4) & ~kLow);
-                    odd[h] = ((w0 >> 4) & kLow) | (w1 & ~kLow);
-                }
+                for (int h = 0; h < 2; ++h) lds<kGroups>(blocks + x * kBytes + value_code_at<D>(8 * h + 2 * t, g), vw[h]);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint32_t b[kParts][2];
+                for (int j = 0; j < kGroups; ++j) {
+                    constexpr uint32_t kLow = 0x0f0f0f0fu;
+                    uint32_t even[2], odd[2];                // [half]: codes of an even dim of two keys to a byte; of an odd dim
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const float x = s[n][2 * h] * vs[h][j], y = s[n][2 * h + 1] * vs[h][j];
-                        const uint32_t w = pack_f16(x, y);
-                        b[0][h] = transposed(w);
-                        if (kParts == 2) b[kParts - 1][h] = transposed(pack_f16_rest(x, y, w));
+                        const uint32_t w0 = vw[h][j / 2], w1 = vw[h][kGroups / 2 + j / 2];
+                        even[h] = (w0 & kLow) | ((w1 << 4) & ~kLow);
+                        odd[h] = ((w0 >> 4) & kLow) | (w1 & ~kLow);
                     }
 #pragma unroll
-                    for (int i = 0; i < kParts; ++i) {
-                        if (j & 1) {
-                            mma_f16(o[n][j][0], two_numbers<2>(even[0]), two_numbers<2>(odd[0]), two_numbers<2>(even[1]), two_numbers<2>(odd[1]), b[i][0], b[i][1]);
-                            mma_f16(o[n][j][1], two_numbers<3>(even[0]), two_numbers<3>(odd[0]), two_numbers<3>(even[1]), two_numbers<3>(odd[1]), b[i][0], b[i][1]);
-                        } else {
-                            mma_f16(o[n][j][0], two_numbers<0>(even[0]), two_numbers<0>(odd[0]), two_numbers<0>(even[1]), two_numbers<0>(odd[1]), b[i][0], b[i][1]);
-                            mma_f16(o[n][j][1], two_numbers<1>(even[0]), two_numbers<1>(odd[0]), two_numbers<1>(even[1]), two_numbers<1>(odd[1]), b[i][0], b[i][1]);
+                    for (int n = 0; n < NT; ++n) {
+                        uint32_t b[kParts][2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float vs = j & 1 ? bf16_high(ws[x][h][j / 2]) : bf16_low(ws[x][h][j / 2]);
+                            const float p0 = s[x][n][2 * h] * vs, p1 = s[x][n][2 * h + 1] * vs;
+                            const uint32_t w = pack_f16(p0, p1);
+                            b[0][h] = transposed(w);
+                            if (kParts == 2) b[kParts - 1][h] = transposed(pack_f16_rest(p0, p1, w));
+                        }
+#pragma unroll
+                        for (int i = 0; i < kParts; ++i) {
+                            if (j & 1) {
+                                mma_f16(o[n][j][0], two_numbers<2>(even[0]), two_numbers<2>(odd[0]), two_numbers<2>(even[1]), two_numbers<2>(odd[1]), b[i][0], b[i][1]);
+                                mma_f16(o[n][j][1], two_numbers<3>(even[0]), two_numbers<3>(odd[0]), two_numbers<3>(even[1]), two_numbers<3>(odd[1]), b[i][0], b[i][1]);
+                            } else {
+                                mma_f16(o[n][j][0], two_numbers<0>(even[0]), two_numbers<0>(odd[0]), two_numbers<0>(even[1]), two_numbers<0>(odd[1]), b[i][0], b[i][1]);
+                                mma_f16(o[n][j][1], two_numbers<1>(even[0]), two_numbers<1>(odd[0]), two_numbers<1>(even[1]), two_numbers<1>(odd[1]), b[i][0], b[i][1]);
+                            }
                         }
                     }
                 }
             }
+            __syncwarp();                                    // the stage has been read
+            if (!given_up) feeder.feed();
         }
 
         // the unit is done, or as much of it as the share has
@@ -551,8 +621,13 @@ kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], x);
-        const bool whole = whole_start && end == p.steps;
-        const int slot = 2 * share + (whole_start ? 1 : 0);
+        float m[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) m[n][i] = slack[n][i] == -INFINITY ? -INFINITY : base[n][i];
+        const bool begins = p.at <= cost, whole = begins && p.end() == p.length;
+        const int slot = 2 * share + (begins ? 1 : 0);
         if (together) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -620,13 +695,10 @@ kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
                     }
                 }
         }
-        if (whole_start && !whole && lane == 0 && (!together || warp == 0)) {
-            const long long more = p.steps - end;             // blocks of the unit in later shares
+        if (begins && !whole && lane == 0 && (!together || warp == 0)) {
+            const long long more = p.length - p.end();        // of the unit in later shares
             a.marks[share] = make_int4(1 + (int)((more + size - 1) / size), p.layer, p.request, p.unit);
         }
-        left -= end - p.step;
-        if (left > 0) line.next_unit(p);
-        whole_start = true;
     }
     if (given_up) {                                          // its copies in flight are given the time to end
         for (; taken < feeder.issued; ++taken) {
@@ -637,6 +709,8 @@ kv4_attn_kernel(Kv4Args args, PagesView pv, Divisor blocks_per_page) {
     }
 }
 
+constexpr int kAtOnce = 4;
+
 // Joins the parts of the unit that begins in share blockIdx.x and goes on in later ones.
 template <typename T, int D>
 __global__ void __launch_bounds__(kMergeThreads)
@@ -646,21 +720,30 @@ kv4_merge_kernel(Kv4Args a, PagesView pv, int cols) {
     const int share = blockIdx.x;
     const int4 mark = a.marks[share];
     if (mark.x > 0) {
-        const int head = mark.w / a.tiles, col0 = (mark.w - head * a.tiles) * cols;
+        const int head = a.tiles.quotient(mark.w), col0 = (mark.w - head * (int)a.tiles.d) * cols;
         for (int i = threadIdx.x; i < cols * (D / 4); i += kMergeThreads) {
             const int c = i / (D / 4), d = i % (D / 4) * 4, column = col0 + c;
             if (column >= a.columns) continue;
             float top = -INFINITY, sum = 0.f;
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k = 0; k < mark.x; ++k) {
-                const size_t slot = k == 0 ? 2 * (size_t)share + 1 : 2 * (size_t)(share + k);
-                const float m = a.part_ml[slot * 2 * cols + c], l = a.part_ml[slot * 2 * cols + cols + c];
-                const float4 y = *reinterpret_cast<const float4*>(a.part_o + (slot * cols + c) * D + d);
-                if (m == -INFINITY && l == 0.f) continue;
-                const float to = fmaxf(top, m), f0 = top == to ? 1.f : exp2f(top - to), f1 = m == to || m == -INFINITY ? 1.f : exp2f(m - to);
-                sum = fmaf(sum, f0, l * f1);
-                x.x = fmaf(x.x, f0, y.x * f1), x.y = fmaf(x.y, f0, y.y * f1), x.z = fmaf(x.z, f0, y.z * f1), x.w = fmaf(x.w, f0, y.w * f1);
-                top = to;
+            for (int k0 = 0; k0 < mark.x; k0 += kAtOnce) {    // that many parts' loads are under way together
+                float m[kAtOnce], l[kAtOnce];
+                float4 y[kAtOnce];
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    const int part = min(k0 + k, mark.x - 1);
+                    const size_t slot = part == 0 ? 2 * (size_t)share + 1 : 2 * (size_t)(share + part);
+                    m[k] = a.part_ml[slot * 2 * cols + c], l[k] = a.part_ml[slot * 2 * cols + cols + c];
+                    y[k] = *reinterpret_cast<const float4*>(a.part_o + (slot * cols + c) * D + d);
+                }
+#pragma unroll
+                for (int k = 0; k < kAtOnce; ++k) {
+                    if (k0 + k >= mark.x || (m[k] == -INFINITY && l[k] == 0.f)) continue;
+                    const float to = fmaxf(top, m[k]), f0 = top == to ? 1.f : exp2f(top - to), f1 = m[k] == to || m[k] == -INFINITY ? 1.f : exp2f(m[k] - to);
+                    sum = fmaf(sum, f0, l[k] * f1);
+                    x.x = fmaf(x.x, f0, y[k].x * f1), x.y = fmaf(x.y, f0, y[k].y * f1), x.z = fmaf(x.z, f0, y[k].z * f1), x.w = fmaf(x.w, f0, y[k].w * f1);
+                    top = to;
+                }
             }
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
             store4<T>(out_row<T, D>(a, pv.n_requests, mark.y, mark.z, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
@@ -683,7 +766,7 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
     c.tiles = (c.columns + 8 * c.nt - 1) / (8 * c.nt);
     c.ctas = sm_count() * (c.nt == 1 ? 2 : 1);
     const double units = (double)n_layers * p->n_requests * g->n_kv_heads * c.tiles;
-    c.warps_per_share = units >= 2.0 * c.ctas * kWarps ? 1 : kWarps;
+    c.warps_per_share = units >= FACTOR * c.ctas * kWarps ? 1 : kWarps;
     c.n_shares = c.warps_per_share == 1 ? c.ctas * kWarps : c.ctas;
     return c;
 }
@@ -697,32 +780,32 @@ int check_attn(const cf_geom* geom, const cf_pages* pages, int q_len, int n_laye
     if (q_len <= 0 || n_layers <= 0 || n_layers > 65535) return CF_ERR_INVALID_ARG;
     const long long columns = (long long)geom->n_q_heads / geom->n_kv_heads * q_len;
     const long long tiles = (columns + 7) / 8;
-    if (columns > (1 << 24) || tiles * geom->n_kv_heads * ((long long)pages->table_cols * (pages->page_rows / 16) + 1) > INT_MAX)
-        return CF_ERR_INVALID_ARG;                // a request's blocks are counted in 32 bits
+    if (columns > (1 << 24) || tiles * geom->n_kv_heads * ((long long)pages->table_cols * (pages->page_rows / 16) / kStepBlocks + 2 + kMostCost) > INT_MAX)
+        return CF_ERR_INVALID_ARG;                // a request's part of the line is counted in 32 bits
     return CF_OK;
 }
 
 size_t attn_smem(int head_dim, int nt) {
-    return (size_t)kWarps * kStages * block_bytes(head_dim) + (size_t)kWarps * 8 * nt * (head_dim + 4) * 4 + 2 * (size_t)kWarps * 8 * nt * 4 +
+    return (size_t)kWarps * kStages * kStepBlocks * block_bytes(head_dim) + (size_t)kWarps * 8 * nt * (head_dim + 4) * 4 + 2 * (size_t)kWarps * 8 * nt * 4 +
            (size_t)kWarps * kStages * 8;
 }
 
 template <typename T, int D, int NT>
-int launch_attn(const Kv4Args& a, const PagesView& pv, Divisor blocks_per_page, int ctas, cudaStream_t stream) {
+int launch_attn(const Kv4Args& a, const PagesView& pv, int ctas, cudaStream_t stream) {
     static PerDeviceOnce once;
     const size_t smem = attn_smem(D, NT);
     const int rc = configure_smem_once(once, kv4_attn_kernel<T, D, NT>, (int)smem);
     if (rc != CF_OK) return rc;
-    const int err = launch_chained(kv4_attn_kernel<T, D, NT>, dim3((unsigned)ctas), kThreads, smem, stream, a, pv, blocks_per_page);
+    const int err = launch_chained(kv4_attn_kernel<T, D, NT>, dim3((unsigned)ctas), kThreads, smem, stream, a, pv);
     if (err != CF_OK) return err;
     return launch_chained(kv4_merge_kernel<T, D>, dim3((unsigned)a.n_shares), kMergeThreads, 0, stream, a, pv, 8 * NT);
 }
 
 template <typename T>
-int launch_attn_typed(const Kv4Args& a, const PagesView& pv, Divisor blocks_per_page, const Cut& c, int head_dim, cudaStream_t stream) {
+int launch_attn_typed(const Kv4Args& a, const PagesView& pv, const Cut& c, int head_dim, cudaStream_t stream) {
     if (head_dim == 128)
-        return c.nt == 1 ? launch_attn<T, 128, 1>(a, pv, blocks_per_page, c.ctas, stream) : launch_attn<T, 128, 2>(a, pv, blocks_per_page, c.ctas, stream);
-    return c.nt == 1 ? launch_attn<T, 64, 1>(a, pv, blocks_per_page, c.ctas, stream) : launch_attn<T, 64, 2>(a, pv, blocks_per_page, c.ctas, stream);
+        return c.nt == 1 ? launch_attn<T, 128, 1>(a, pv, c.ctas, stream) : launch_attn<T, 128, 2>(a, pv, c.ctas, stream);
+    return c.nt == 1 ? launch_attn<T, 64, 1>(a, pv, c.ctas, stream) : launch_attn<T, 64, 2>(a, pv, c.ctas, stream);
 }
 
 }  // namespace
@@ -767,15 +850,16 @@ int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, in
     a.marks = reinterpret_cast<int4*>(w + round_up(rows * geom->head_dim * 4) + round_up(rows * 8));
     a.q_layer_stride = q_layer_stride, a.kv4_layer_stride = kv4_layer_stride, a.out_layer_stride = out_layer_stride;
     a.n_layers = n_layers, a.q_len = q_len, a.n_q_heads = geom->n_q_heads, a.n_kv_heads = geom->n_kv_heads;
-    a.group = geom->n_q_heads / geom->n_kv_heads, a.columns = c.columns, a.tiles = c.tiles;
+    a.columns = c.columns;
+    a.group = Divisor(geom->n_q_heads / geom->n_kv_heads), a.tiles = Divisor(c.tiles), a.blocks_per_page = Divisor(pages->page_rows / kBlockRows);
     a.n_shares = c.n_shares, a.warps_per_share = c.warps_per_share;
-    a.least_share = c.warps_per_share == 1 ? 4 : 2 * kWarps;
+    a.least_share = c.warps_per_share == 1 ? LEAST1 : LEAST;
+    a.unit_cost = c.warps_per_share == 1 ? COST1 : COST;
     a.scale_log2 = scale * kLog2e;
     const PagesView pv = make_pages_view(pages);
-    const Divisor blocks_per_page(pages->page_rows / kBlockRows);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return geom->dtype == CF_BF16 ? launch_attn_typed<__nv_bfloat16>(a, pv, blocks_per_page, c, geom->head_dim, s)
-                                  : launch_attn_typed<float>(a, pv, blocks_per_page, c, geom->head_dim, s);
+    return geom->dtype == CF_BF16 ? launch_attn_typed<__nv_bfloat16>(a, pv, c, geom->head_dim, s)
+                                  : launch_attn_typed<float>(a, pv, c, geom->head_dim, s);
 }
 
 }  // extern "C"
