@@ -56,6 +56,9 @@ constexpr int kMostCost = 32;                     // of a unit, in steps
 #define COST 16
 #endif
 
+// Query columns of a unit.
+__host__ __device__ constexpr int tile_columns(int head_dim, int nt, bool few) { return few ? 8 / (head_dim / 32) : 8 * nt; }
+
 struct Kv4Args {
     const void* q;
     const unsigned char* kv4;
@@ -182,7 +185,7 @@ struct Line {
 };
 
 // The copies of a warp's steps: it takes every stride-th step from `first` on of each unit of its share.  The walk lies in shared
-// memory: it is looked at once in sixteen steps.
+// memory: it is looked at once in 32 steps.
 template <int D>
 struct Feeder {
     static constexpr int kBytes = block_bytes(D);
@@ -191,15 +194,21 @@ struct Feeder {
     const Line& line;
     Walk* walk;
     int* next;                                    // the unit's next step to look up
-    int first, stride;
-    int ready, used;                              // steps whose addresses the lanes hold, two lanes a step; how many of them were issued
-    const unsigned char* address;                 // lane l's block, nullptr for a block behind the rows
+    int first, stride, lane;
+    int ready, used;                              // steps that the lanes have looked up, one each; how many of them were issued
+    const unsigned char* address;                 // a lane's step: its first block,
+    int second;                                   // and how many blocks behind that its second one lies (0: it has none)
     uint32_t ring, bars;
     unsigned issued;
     bool ended;
 
+    __device__ __forceinline__ int page_of(int request, int rows, int column) const {
+        const int page = pv.table[(size_t)request * pv.table_cols + column];
+        if ((unsigned)page < (unsigned)pv.n_pages) return page;
+        if (rows > 0) atomicCAS(pv.status, 0, CF_ERR_RANGE);       // a request without rows has no pages
+        return 0;
+    }
     __device__ __forceinline__ void look_up() {
-        const int lane = threadIdx.x & 31;
         __syncwarp();
         Walk p = *walk;
         int step = *next;
@@ -209,19 +218,15 @@ struct Feeder {
             const int last = p.last_step(line.cost);
             const int n = step < last ? (last - step + stride - 1) / stride : 0;
             if (n > 0) {
-                ready = min(16, n);
-                address = nullptr;
-                const int block = kStepBlocks * (step + (lane >> 1) * stride) + (lane & 1);
-                if ((lane >> 1) < ready && (block == 0 || block * kBlockRows < p.rows)) {
-                    const int column = a.blocks_per_page.quotient(block);
-                    int page = pv.table[(size_t)p.request * pv.table_cols + column];
-                    if ((unsigned)page >= (unsigned)pv.n_pages) {
-                        if (p.rows > 0) atomicCAS(pv.status, 0, CF_ERR_RANGE);   // a request without rows has no pages
-                        page = 0;
-                    }
-                    const int head = a.tiles.quotient(p.unit);
-                    address = a.kv4 + (size_t)p.layer * a.kv4_layer_stride +
-                              (((size_t)page * a.n_kv_heads + head) * a.blocks_per_page.d + (block - column * (int)a.blocks_per_page.d)) * kBytes;
+                ready = min(32, n);
+                if (lane < ready) {
+                    const int per_page = (int)a.blocks_per_page.d, block = kStepBlocks * (step + lane * stride);
+                    const int column = a.blocks_per_page.quotient(block), in_page = block - column * per_page;
+                    const int head = a.tiles.quotient(p.unit), page = page_of(p.request, p.rows, column);
+                    address = a.kv4 + (size_t)p.layer * a.kv4_layer_stride + (((size_t)page * a.n_kv_heads + head) * per_page + in_page) * kBytes;
+                    second = (block + 1) * kBlockRows >= p.rows ? 0 : 1;
+                    if (second != 0 && in_page + 1 == per_page)
+                        second = (page_of(p.request, p.rows, column + 1) - page) * a.n_kv_heads * per_page - in_page;
                 }
                 step += ready * stride;
                 break;
@@ -232,6 +237,10 @@ struct Feeder {
         if (lane == 0) *walk = p, *next = step;
         __syncwarp();
     }
+    __device__ __forceinline__ static void copy(uint32_t to, const unsigned char* from, uint32_t bytes, uint32_t bar) {
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
+                     : "memory");
+    }
     // Issues the next step's copies into the stage that was read last.
     __device__ __forceinline__ void feed() {
         if (used == ready) {
@@ -240,18 +249,11 @@ struct Feeder {
             ended = ready == 0;
             if (ended) return;
         }
-        const int lane = threadIdx.x & 31;
-        const uint32_t stage = issued % kStages;
-        if ((lane >> 1) == used) {
-            const uint32_t bar = bars + 8 * stage;
-            if (address) {
-                mbar_expect_tx(bar, kBytes);
-                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(ring + (stage * kStepBlocks + (lane & 1)) * kBytes),
-                             "l"(address), "r"(kBytes), "r"(bar)
-                             : "memory");
-            } else {
-                tc::mbar_arrive(bar);
-            }
+        if (lane == used) {
+            const uint32_t stage = issued % kStages, bar = bars + 8 * stage, to = ring + stage * kStepBlocks * kBytes;
+            mbar_expect_tx(bar, second != 0 ? 2 * kBytes : kBytes);
+            copy(to, address, second == 1 ? 2 * kBytes : kBytes, bar);
+            if (second != 0 && second != 1) copy(to + kBytes, address + (long long)second * kBytes, kBytes, bar);
         }
         ++used;
         ++issued;
@@ -274,7 +276,7 @@ __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, float a,
 
 // Results of a column: where they go, by the column's number within the kv head (token-major).
 template <typename T, int D>
-__device__ __forceinline__ T* out_row(const Kv4Args& a, int n_requests, int layer, int request, int head, int column) {
+__device__ __forceinline__ T* out_row(const Kv4Args& a, int layer, int request, int head, int column) {
     const int token = a.group.quotient(column), h = head * (int)a.group.d + a.group.remainder(column);
     return static_cast<T*>(a.out) + (size_t)layer * a.out_layer_stride + (((size_t)request * a.q_len + token) * a.n_q_heads + h) * D;
 }
@@ -284,14 +286,18 @@ __device__ __forceinline__ void store_lse(const Kv4Args& a, int n_requests, int 
     a.lse[(((size_t)layer * n_requests + request) * a.n_q_heads + h) * a.q_len + token] = l > 0.f || l != l ? m * kLn2 + logf(l) : -INFINITY;
 }
 
-template <typename T, int D, int NT>
+// FEW: the query columns times the groups fit the eight columns of a matrix product, which then has a column per (query, group):
+// one chain of products for all groups, and one set of probabilities instead of one per group.
+template <typename T, int D, int NT, bool FEW>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
 kv4_attn_kernel(Kv4Args args, PagesView pv) {
     chain_next();
     constexpr int kBytes = block_bytes(D);
     constexpr int kRing = kStages * kStepBlocks * kBytes;    // of a warp
     constexpr int kGroups = D / 32;
-    constexpr int kCols = 8 * NT;
+    constexpr int kCols = tile_columns(D, NT, FEW);          // query columns of a unit
+    constexpr int kOwn = FEW ? 1 : 2 * NT;                   // of which a lane has the logits of this many
+    constexpr int kScaleWords = FEW ? 1 : kGroups / 2;       // scales of a key that a lane reads, two to a word
     constexpr int kParts = IsF32<T>::value ? 2 : 1;          // fp16 numbers per query or probability
     constexpr int kOStride = D + 4;                          // floats between columns in shared memory: no bank conflicts
     extern __shared__ __align__(128) unsigned char smem[];
@@ -304,7 +310,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
     __shared__ int s_next[kWarps];
     __shared__ volatile int s_abort;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    if (lane < kStages) mbar_init(smem_u32(s_bars + warp * kStages + lane), kStepBlocks);
+    if (lane < kStages) mbar_init(smem_u32(s_bars + warp * kStages + lane), 1);
     if (tid == 0) s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     __syncthreads();
@@ -329,30 +335,39 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
     const int first_step = together ? warp : 0, stride = together ? kWarps : 1;
     const uint32_t ring = smem_u32(s_ring) + warp * kRing, bars = smem_u32(s_bars + warp * kStages);
     if (lane == 0) s_walk[warp] = p, s_next[warp] = p.first_step(cost) + first_step;
-    Feeder<D> feeder = {pv, a, line, s_walk + warp, s_next + warp, first_step, stride, 0, 0, nullptr, ring, bars, 0u, false};
+    Feeder<D> feeder = {pv, a, line, s_walk + warp, s_next + warp, first_step, stride, lane, 0, 0, nullptr, 0, ring, bars, 0u, false};
 #pragma unroll 1
     for (int i = 0; i < kStages; ++i) feeder.feed();
     unsigned taken = 0;                                      // steps that were waited for
     bool given_up = false;
+    const uint32_t code_lane = g * (D / 2) + t * (D / 8);    // a lane's codes within the rows of its half, keys and values alike
+    const uint32_t scale_lane = g * (D / 16) + (FEW ? 4 * t % (D / 16) : 0);
 
     for (; p.left > 0; line.next_unit(p)) {                  // a unit, or the share's part of one
         const int start = p.first_step(cost), last = p.last_step(cost);
         if (last <= start) continue;                         // the unit's first step is the next share's
         const int head = a.tiles.quotient(p.unit), col0 = (p.unit - head * (int)a.tiles.d) * kCols;
-        // the queries: lane (g, t) holds dims 32 j + 8 t .. + 7 of column g of every tile of eight
+        // the queries: lane (g, t) holds dims 32 j + 8 t .. + 7 of its column of the products, g (FEW: those of group g % kGroups of
+        // query column g / kGroups, zeros elsewhere)
         uint32_t qf[NT][kParts][kGroups][2][2];
-        float cs[NT][2];                                     // what turns sums of codes into base-2 logits, columns 2t and 2t + 1
-        int sees[NT][2];                                     // rows that they see
+        float cs[kOwn];                                      // what turns sums of codes into base-2 logits
+        int sees[kOwn];                                      // rows that the lane's queries see
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int column = col0 + 8 * n + g;
-            float x[kGroups][8];
+            const int column = col0 + (FEW ? g / kGroups : 8 * n + g);
+            constexpr int kLoads = FEW ? 1 : kGroups;
+            float x[kLoads][8];
             uint32_t amax = 0;
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
             if (column < a.columns) {
                 const int token = a.group.quotient(column), h = head * (int)a.group.d + a.group.remainder(column);
-                const T* q = static_cast<const T*>(a.q) + (size_t)p.layer * a.q_layer_stride + (((size_t)p.request * a.q_len + token) * a.n_q_heads + h) * D + 8 * t;
+                const T* q = static_cast<const T*>(a.q) + (size_t)p.layer * a.q_layer_stride + (((size_t)p.request * a.q_len + token) * a.n_q_heads + h) * D +
+                             8 * t + (FEW ? 32 * (g % kGroups) : 0);
 #pragma unroll
-                for (int j = 0; j < kGroups; ++j) {
+                for (int j = 0; j < kLoads; ++j) {
                     uint32_t w[4 * kParts];
 #pragma unroll
                     for (int i = 0; i < kParts; ++i) *reinterpret_cast<uint4*>(w + 4 * i) = *reinterpret_cast<const uint4*>(q + 32 * j + 4 * i);
@@ -362,14 +377,9 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                         amax = max(amax, __float_as_uint(x[j][i]) & 0x7fffffffu);
                     }
                 }
-            } else {
-#pragma unroll
-                for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
             }
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 1));
-            amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
+#pragma unroll
+            for (int y = 1; y < (FEW ? 4 * kGroups : 4); y <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, y));
             int e = amax == 0 || amax >= 0x7f800000u ? 0 : (int)(amax >> 23) - 127;      // the largest magnitude comes to lie in [1, 2)
             e = max(-126, min(126, e));
             const float down = __int_as_float((127 - e) << 23), up = __int_as_float((127 + e) << 23);
@@ -377,33 +387,32 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
             for (int j = 0; j < kGroups; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float lo = x[j][2 * i] * down, hi = x[j][2 * i + 1] * down;
+                    const bool mine = !FEW || j == g % kGroups;
+                    const float lo = mine ? x[j % kLoads][2 * i] * down : 0.f, hi = mine ? x[j % kLoads][2 * i + 1] * down : 0.f;
                     qf[n][0][j][i / 2][i & 1] = pack_f16(lo, hi);
                     if (kParts == 2) qf[n][kParts - 1][j][i / 2][i & 1] = pack_f16_rest(lo, hi, qf[n][0][j][i / 2][i & 1]);
                 }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                cs[n][i] = a.scale_log2 * __shfl_sync(0xffffffffu, up, (2 * t + i) * 4);
-                const int mine = col0 + 8 * n + 2 * t + i;
-                sees[n][i] = mine < a.columns ? p.rows - a.q_len + 1 + a.group.quotient(mine) : p.rows;
+            for (int i = 0; i < (FEW ? 1 : 2); ++i) {
+                cs[FEW ? 0 : 2 * n + i] = a.scale_log2 * __shfl_sync(0xffffffffu, up, (2 * t + i) * 4);
+                const int mine = col0 + (FEW ? 2 * t / kGroups : 8 * n + 2 * t + i);
+                sees[FEW ? 0 : 2 * n + i] = mine < a.columns ? p.rows - a.q_len + 1 + a.group.quotient(mine) : p.rows;
             }
         }
         const int all_see = p.rows - a.q_len + 1 + a.group.quotient(col0);       // what the tile's first column sees, the fewest
 
         // base: what logits are taken from (the running maximum, 0 before there is one); slack: how far above it they may lie
-        float o[NT][kGroups][2][4], base[NT][2], slack[NT][2], l[NT][2];
+        float o[NT][kGroups][2][4], base[kOwn], slack[kOwn], l[kOwn];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < kGroups; ++j)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) o[n][j][i][k] = 0.f;
-            base[n][0] = base[n][1] = 0.f;
-            slack[n][0] = slack[n][1] = -INFINITY;
-            l[n][0] = l[n][1] = 0.f;
-        }
+#pragma unroll
+        for (int c = 0; c < kOwn; ++c) base[c] = 0.f, slack[c] = -INFINITY, l[c] = 0.f;
         int exponent = kLeastExponent;                       // values are taken in units of 2^(exponent - kHead)
         uint32_t scale_limit = (uint32_t)(127 + exponent) * 0x00800080u;   // 2^exponent as bf16, twice
         float scale_down = exp2f((float)(kHead - exponent));
@@ -412,51 +421,64 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
             const uint32_t stage = taken % kStages, blocks = ring + stage * kStepBlocks * kBytes;
             if (!given_up && !tc::mbar_wait(bars + 8 * stage, taken / kStages & 1, &s_abort)) given_up = true;
             if (!given_up) ++taken;
-            // S^T of 32 keys
-            float s[kStepBlocks][NT][4];
+            // S^T of 32 keys: s[block][half][own column]
+            float s[kStepBlocks][2][kOwn];
 #pragma unroll
             for (int x = 0; x < kStepBlocks; ++x) {
-                const uint32_t block = blocks + x * kBytes;
-                uint32_t k0[kGroups], k1[kGroups], ks0[kGroups / 2], ks1[kGroups / 2];
-                lds<kGroups>(block + key_code_at<D>(g) + t * (D / 8), k0);
-                lds<kGroups>(block + key_code_at<D>(g + 8) + t * (D / 8), k1);
-                lds<kGroups / 2>(block + key_scale_at<D>(g), ks0);
-                lds<kGroups / 2>(block + key_scale_at<D>(g + 8), ks1);
+                const uint32_t codes = blocks + x * kBytes + code_lane, scales = blocks + x * kBytes + scale_lane;
+                uint32_t k0[kGroups], k1[kGroups], ks[2][kScaleWords];
+                lds<kGroups>(codes + key_code_at<D>(0), k0);
+                lds<kGroups>(codes + key_code_at<D>(8), k1);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) lds<kScaleWords>(scales + key_scale_at<D>(8 * h), ks[h]);
+                float c[NT][4];
 #pragma unroll
                 for (int j = 0; j < kGroups; ++j) {
                     const uint32_t a00 = two_numbers<0>(k0[j]), a10 = two_numbers<0>(k1[j]), a20 = two_numbers<1>(k0[j]), a30 = two_numbers<1>(k1[j]);
                     const uint32_t a01 = two_numbers<2>(k0[j]), a11 = two_numbers<2>(k1[j]), a21 = two_numbers<3>(k0[j]), a31 = two_numbers<3>(k1[j]);
-                    const float f0 = j & 1 ? bf16_high(ks0[j / 2]) : bf16_low(ks0[j / 2]), f1 = j & 1 ? bf16_high(ks1[j / 2]) : bf16_low(ks1[j / 2]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        float c[4];
-                        mma_f16_first(c, a00, a10, a20, a30, qf[n][0][j][0][0], qf[n][0][j][0][1]);
-                        mma_f16(c, a01, a11, a21, a31, qf[n][0][j][1][0], qf[n][0][j][1][1]);
+                        if (FEW && j > 0) mma_f16(c[n], a00, a10, a20, a30, qf[n][0][j][0][0], qf[n][0][j][0][1]);
+                        else mma_f16_first(c[n], a00, a10, a20, a30, qf[n][0][j][0][0], qf[n][0][j][0][1]);
+                        mma_f16(c[n], a01, a11, a21, a31, qf[n][0][j][1][0], qf[n][0][j][1][1]);
                         if (kParts == 2) {
-                            mma_f16(c, a00, a10, a20, a30, qf[n][kParts - 1][j][0][0], qf[n][kParts - 1][j][0][1]);
-                            mma_f16(c, a01, a11, a21, a31, qf[n][kParts - 1][j][1][0], qf[n][kParts - 1][j][1][1]);
+                            mma_f16(c[n], a00, a10, a20, a30, qf[n][kParts - 1][j][0][0], qf[n][kParts - 1][j][0][1]);
+                            mma_f16(c[n], a01, a11, a21, a31, qf[n][kParts - 1][j][1][0], qf[n][kParts - 1][j][1][1]);
                         }
-                        if (j == 0) {
-                            s[x][n][0] = c[0] * f0, s[x][n][1] = c[1] * f0, s[x][n][2] = c[2] * f1, s[x][n][3] = c[3] * f1;
-                        } else {
-                            s[x][n][0] = fmaf(c[0], f0, s[x][n][0]), s[x][n][1] = fmaf(c[1], f0, s[x][n][1]);
-                            s[x][n][2] = fmaf(c[2], f1, s[x][n][2]), s[x][n][3] = fmaf(c[3], f1, s[x][n][3]);
+                        if (!FEW) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const float f = j & 1 ? bf16_high(ks[h][j / 2 % kScaleWords]) : bf16_low(ks[h][j / 2 % kScaleWords]);
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    float& y = s[x][h][(2 * n + i) % kOwn];
+                                    y = j == 0 ? c[n][2 * h + i] * f : fmaf(c[n][2 * h + i], f, y);
+                                }
+                            }
                         }
                     }
                 }
+                if (FEW) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float y = fmaf(c[0][2 * h + 1], bf16_high(ks[h][0]), c[0][2 * h] * bf16_low(ks[h][0]));
+                        if (kGroups == 4) y += __shfl_xor_sync(0xffffffffu, y, 1);
+                        s[x][h][0] = y;
+                    }
+                }
             }
-            uint32_t ws[kStepBlocks][2][kGroups / 2];        // scales of keys g and g + 8
+            uint32_t ws[kStepBlocks][2][kScaleWords];        // scales of the values of keys g and g + 8
 #pragma unroll
             for (int x = 0; x < kStepBlocks; ++x)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) lds<kGroups / 2>(blocks + x * kBytes + value_scale_at<D>(g + 8 * h), ws[x][h]);
+                for (int h = 0; h < 2; ++h) lds<kScaleWords>(blocks + x * kBytes + scale_lane + value_scale_at<D>(8 * h), ws[x][h]);
 
 #pragma unroll
             for (int x = 0; x < kStepBlocks; ++x)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[x][n][i] = fmaf(s[x][n][i], cs[n][i & 1], -base[n][i & 1]);
+                    for (int c = 0; c < kOwn; ++c) s[x][h][c] = fmaf(s[x][h][c], cs[c], -base[c]);
             if ((step + 1) * kStepRows > all_see) {          // some query does not see some of the keys
                 bool nan = false;
 #pragma unroll
@@ -465,19 +487,17 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                     for (int h = 0; h < 2; ++h) {
                         const int row = step * kStepRows + x * kBlockRows + g + 8 * h;
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                        for (int c = 0; c < kOwn; ++c)
+                            if (row >= sees[c]) s[x][h][c] = -INFINITY;
 #pragma unroll
-                            for (int i = 0; i < 2; ++i)
-                                if (row >= sees[n][i]) s[x][n][2 * h + i] = -INFINITY;
-#pragma unroll
-                        for (int i = 0; i < kGroups / 2; ++i) {
+                        for (int i = 0; i < kScaleWords; ++i) {
                             if (row >= p.rows) ws[x][h][i] = 0u;     // rows behind the last may hold anything
                             nan |= bf16_low(ws[x][h][i]) != bf16_low(ws[x][h][i]) || bf16_high(ws[x][h][i]) != bf16_high(ws[x][h][i]);
                         }
                     }
                 if (__any_sync(0xffffffffu, nan)) {          // a NaN reaches the queries that see its row, and no others
 #pragma unroll
-                    for (int j = 0; j < kGroups; ++j) {
+                    for (int j = 0; j < 2 * kScaleWords; ++j) {
                         bool is_nan[kStepBlocks][2];
 #pragma unroll
                         for (int x = 0; x < kStepBlocks; ++x)
@@ -488,33 +508,37 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                                 if (is_nan[x][h]) ws[x][h][j / 2] &= j & 1 ? 0x0000ffffu : 0xffff0000u;
                             }
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                        for (int c = 0; c < kOwn; ++c) {
+                            bool hit = false;
 #pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                bool hit = false;
+                            for (int x = 0; x < kStepBlocks; ++x)
 #pragma unroll
-                                for (int x = 0; x < kStepBlocks; ++x)
+                                for (int h = 0; h < 2; ++h) hit |= is_nan[x][h] && step * kStepRows + x * kBlockRows + g + 8 * h < sees[c];
+                            // lanes of the same columns: bits t, t + 4, ...
+                            if (__ballot_sync(0xffffffffu, hit) & (0x11111111u << t)) {
+                                const float bad = __int_as_float(0x7fffffff);
 #pragma unroll
-                                    for (int h = 0; h < 2; ++h) hit |= is_nan[x][h] && step * kStepRows + x * kBlockRows + g + 8 * h < sees[n][i];
-                                // lanes of the same columns: bits t, t + 4, ...
-                                if (__ballot_sync(0xffffffffu, hit) & (0x11111111u << t))
+                                for (int k = 0; k < 2; ++k) {
+                                    if (!FEW) {
+                                        o[c / 2][j % kGroups][k][c & 1] = o[c / 2][j % kGroups][k][(c & 1) + 2] = bad;
+                                    } else {
 #pragma unroll
-                                    for (int k = 0; k < 2; ++k) o[n][j][k][i] = o[n][j][k][i + 2] = __int_as_float(0x7fffffff);
+                                        for (int jj = 0; jj < kGroups; ++jj) o[0][jj][k][j & 1] = o[0][jj][k][(j & 1) + 2] = bad;
+                                    }
+                                }
                             }
+                        }
                     }
                 }
             }
             bool raise = false;
+#pragma unroll
+            for (int c = 0; c < kOwn; ++c) raise |= fmaxf(fmaxf(s[0][0][c], s[0][1][c]), fmaxf(s[1][0][c], s[1][1][c])) > slack[c];
             uint32_t most = scale_limit;                     // scales order as integers
 #pragma unroll
-            for (int x = 0; x < kStepBlocks; ++x) {
+            for (int x = 0; x < kStepBlocks; ++x)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) raise |= s[x][n][i] > slack[n][i & 1];
-#pragma unroll
-                for (int i = 0; i < kGroups / 2; ++i) most = __vmaxu2(most, __vmaxu2(ws[x][0][i], ws[x][1][i]));
-            }
+                for (int i = 0; i < kScaleWords; ++i) most = __vmaxu2(most, __vmaxu2(ws[x][0][i], ws[x][1][i]));
             raise |= most != scale_limit;
             if (__any_sync(0xffffffffu, raise)) {
                 float vmax = 0.f;
@@ -523,9 +547,9 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int i = 0; i < kGroups / 2; ++i) vmax = fmaxf(vmax, fmaxf(bf16_low(ws[x][h][i]), bf16_high(ws[x][h][i])));
+                        for (int i = 0; i < kScaleWords; ++i) vmax = fmaxf(vmax, fmaxf(bf16_low(ws[x][h][i]), bf16_high(ws[x][h][i])));
 #pragma unroll
-                for (int y = 4; y < 32; y <<= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, y));
+                for (int y = 1; y < 32; y <<= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xffffffffu, vmax, y));
                 float f = 1.f;
                 if (vmax > bf16_low(scale_limit)) {
                     const int e = min((int)(__float_as_uint(vmax) >> 23) - 126, 127);
@@ -535,46 +559,48 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                     scale_down = exp2f((float)(kHead - e));
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int c = 0; c < kOwn; ++c) {
+                    float y = -INFINITY;                     // above `base`
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float y = -INFINITY;                 // above `base`
+                    for (int x = 0; x < kStepBlocks; ++x) y = fmaxf(y, fmaxf(s[x][0][c], s[x][1][c]));
 #pragma unroll
-                        for (int x = 0; x < kStepBlocks; ++x) y = fmaxf(y, fmaxf(s[x][n][i], s[x][n][i + 2]));
+                    for (int k = 4; k < 32; k <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, k));
+                    float r = 1.f;
+                    if (slack[c] != -INFINITY) y = fmaxf(y, 0.f), r = exp2_fast(-y);
+                    if (y != -INFINITY) {                    // otherwise the column has seen nothing yet
+                        base[c] += y;
+                        slack[c] = kSlack;
 #pragma unroll
-                        for (int k = 4; k < 32; k <<= 1) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, k));
-                        float r = 1.f;
-                        if (slack[n][i] != -INFINITY) y = fmaxf(y, 0.f), r = exp2_fast(-y);
-                        if (y != -INFINITY) {                // otherwise the column has seen nothing yet
-                            base[n][i] += y;
-                            slack[n][i] = kSlack;
-#pragma unroll
-                            for (int x = 0; x < kStepBlocks; ++x) s[x][n][i] -= y, s[x][n][i + 2] -= y;
-                        }
-                        l[n][i] *= r;
-#pragma unroll
-                        for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) o[n][j][k][i] *= r * f, o[n][j][k][i + 2] *= r * f;
+                        for (int x = 0; x < kStepBlocks; ++x) s[x][0][c] -= y, s[x][1][c] -= y;
                     }
+                    l[c] *= r;
+#pragma unroll
+                    for (int j = 0; j < kGroups; ++j)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            o[c / 2][j][k][c & 1] *= r * f, o[c / 2][j][k][(c & 1) + 2] *= r * f;
+                            if (FEW) o[0][j][k][1] *= r * f, o[0][j][k][3] *= r * f;
+                        }
+                }
             }
             // the probabilities
 #pragma unroll
             for (int x = 0; x < kStepBlocks; ++x)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float y = exp2_fast(s[x][n][i]);
-                        l[n][i & 1] += y;
-                        s[x][n][i] = y * scale_down;
+                    for (int c = 0; c < kOwn; ++c) {
+                        const float y = exp2_fast(s[x][h][c]);
+                        l[c] += y;
+                        s[x][h][c] = y * scale_down;
                     }
             // O^T += V^T P^T, group by group
 #pragma unroll
             for (int x = 0; x < kStepBlocks; ++x) {
                 uint32_t vw[2][kGroups];                     // [half]: groups two by two of an even key's codes, of an odd one's
+                uint32_t b[NT][kParts][2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) lds<kGroups>(blocks + x * kBytes + value_code_at<D>(8 * h + 2 * t, g), vw[h]);
+                for (int h = 0; h < 2; ++h) lds<kGroups>(blocks + x * kBytes + code_lane + value_code_at<D>(8 * h, 0), vw[h]);
 #pragma unroll
                 for (int j = 0; j < kGroups; ++j) {
                     constexpr uint32_t kLow = 0x0f0f0f0fu;
@@ -587,23 +613,25 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        uint32_t b[kParts][2];
+                        if (!FEW || j == 0) {
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float vs = j & 1 ? bf16_high(ws[x][h][j / 2]) : bf16_low(ws[x][h][j / 2]);
-                            const float p0 = s[x][n][2 * h] * vs, p1 = s[x][n][2 * h + 1] * vs;
-                            const uint32_t w = pack_f16(p0, p1);
-                            b[0][h] = transposed(w);
-                            if (kParts == 2) b[kParts - 1][h] = transposed(pack_f16_rest(p0, p1, w));
+                            for (int h = 0; h < 2; ++h) {
+                                const uint32_t w = ws[x][h][FEW ? 0 : j / 2 % kScaleWords];
+                                const float v0 = FEW || !(j & 1) ? bf16_low(w) : bf16_high(w), v1 = FEW ? bf16_high(w) : v0;
+                                const float p0 = s[x][h][2 * n % kOwn] * v0, p1 = s[x][h][(2 * n + 1) % kOwn] * v1;
+                                const uint32_t packed = pack_f16(p0, p1);
+                                b[n][0][h] = transposed(packed);
+                                if (kParts == 2) b[n][kParts - 1][h] = transposed(pack_f16_rest(p0, p1, packed));
+                            }
                         }
 #pragma unroll
                         for (int i = 0; i < kParts; ++i) {
                             if (j & 1) {
-                                mma_f16(o[n][j][0], two_numbers<2>(even[0]), two_numbers<2>(odd[0]), two_numbers<2>(even[1]), two_numbers<2>(odd[1]), b[i][0], b[i][1]);
-                                mma_f16(o[n][j][1], two_numbers<3>(even[0]), two_numbers<3>(odd[0]), two_numbers<3>(even[1]), two_numbers<3>(odd[1]), b[i][0], b[i][1]);
+                                mma_f16(o[n][j][0], two_numbers<2>(even[0]), two_numbers<2>(odd[0]), two_numbers<2>(even[1]), two_numbers<2>(odd[1]), b[n][i][0], b[n][i][1]);
+                                mma_f16(o[n][j][1], two_numbers<3>(even[0]), two_numbers<3>(odd[0]), two_numbers<3>(even[1]), two_numbers<3>(odd[1]), b[n][i][0], b[n][i][1]);
                             } else {
-                                mma_f16(o[n][j][0], two_numbers<0>(even[0]), two_numbers<0>(odd[0]), two_numbers<0>(even[1]), two_numbers<0>(odd[1]), b[i][0], b[i][1]);
-                                mma_f16(o[n][j][1], two_numbers<1>(even[0]), two_numbers<1>(odd[0]), two_numbers<1>(even[1]), two_numbers<1>(odd[1]), b[i][0], b[i][1]);
+                                mma_f16(o[n][j][0], two_numbers<0>(even[0]), two_numbers<0>(odd[0]), two_numbers<0>(even[1]), two_numbers<0>(odd[1]), b[n][i][0], b[n][i][1]);
+                                mma_f16(o[n][j][1], two_numbers<1>(even[0]), two_numbers<1>(odd[0]), two_numbers<1>(even[1]), two_numbers<1>(odd[1]), b[n][i][0], b[n][i][1]);
                             }
                         }
                     }
@@ -615,32 +643,33 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
 
         // the unit is done, or as much of it as the share has
         const float unit_scale = exp2f((float)(exponent - kHead));
+        float m[kOwn];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int c = 0; c < kOwn; ++c) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], x);
-        float m[NT][2];
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) m[n][i] = slack[n][i] == -INFINITY ? -INFINITY : base[n][i];
+            for (int x = 4; x < 32; x <<= 1) l[c] += __shfl_xor_sync(0xffffffffu, l[c], x);
+            m[c] = slack[c] == -INFINITY ? -INFINITY : base[c];
+        }
         const bool begins = p.at <= cost, whole = begins && p.end() == p.length;
         const int slot = 2 * share + (begins ? 1 : 0);
+        // a lane's dims 32 j + 4 g .. + 3 of own column c, where it has them
+        auto has = [&](int j) { return !FEW || t % (kGroups / 2) == j / 2; };
+        auto dims = [&](int c, int j, float f) {
+            const int n = FEW ? 0 : c / 2, i = FEW ? j & 1 : c & 1;
+            return make_float4(o[n][j][0][i] * f, o[n][j][0][i + 2] * f, o[n][j][1][i] * f, o[n][j][1][i + 2] * f);
+        };
+        auto tile_column = [&](int c) { return FEW ? 2 * t / kGroups : 8 * (c / 2) + 2 * t + (c & 1); };
+        const bool first_lane = g == 0 && (!FEW || t % (kGroups / 2) == 0);      // of those that have a column
         if (together) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+            for (int i = 0; i < kOwn; ++i) {
+                const int c = tile_column(i);
+                float* row = s_o + (warp * kCols + c) * kOStride + 4 * g;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int c = 8 * n + 2 * t + i;
-                    float* row = s_o + (warp * kCols + c) * kOStride + 4 * g;
-#pragma unroll
-                    for (int j = 0; j < kGroups; ++j)
-                        *reinterpret_cast<float4*>(row + 32 * j) =
-                            make_float4(o[n][j][0][i] * unit_scale, o[n][j][0][i + 2] * unit_scale, o[n][j][1][i] * unit_scale, o[n][j][1][i + 2] * unit_scale);
-                    if (g == 0) s_m[warp * kCols + c] = m[n][i], s_l[warp * kCols + c] = l[n][i];
-                }
+                for (int j = 0; j < kGroups; ++j)
+                    if (has(j)) *reinterpret_cast<float4*>(row + 32 * j) = dims(i, j, unit_scale);
+                if (first_lane) s_m[warp * kCols + c] = m[i], s_l[warp * kCols + c] = l[i];
+            }
             __syncthreads();
             for (int i = tid; i < kCols * (D / 4); i += kThreads) {
                 const int c = i / (D / 4), d = i % (D / 4) * 4, column = col0 + c;
@@ -651,18 +680,17 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                 float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) {
-                    const float mw = s_m[w * kCols + c], f = mw == -INFINITY ? 0.f : exp2f(mw - top), lw = s_l[w * kCols + c];
+                    const float mw = s_m[w * kCols + c], lw = s_l[w * kCols + c];
                     const float4 y = *reinterpret_cast<const float4*>(s_o + (w * kCols + c) * kOStride + d);
-                    // a warp that saw no key (or only NaN) has m = -inf
-                    if (mw == -INFINITY && lw == 0.f) continue;
-                    const float k = mw == -INFINITY ? 1.f : f;
+                    if (mw == -INFINITY && lw == 0.f) continue;          // a warp that saw no key
+                    const float k = mw == -INFINITY ? 1.f : exp2f(mw - top);     // (one that saw only NaN has no maximum)
                     sum = fmaf(lw, k, sum);
                     x.x = fmaf(y.x, k, x.x), x.y = fmaf(y.y, k, x.y), x.z = fmaf(y.z, k, x.z), x.w = fmaf(y.w, k, x.w);
                 }
                 if (whole) {
                     if (column < a.columns) {
                         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                        store4<T>(out_row<T, D>(a, pv.n_requests, p.layer, p.request, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+                        store4<T>(out_row<T, D>(a, p.layer, p.request, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
                         if (d == 0) store_lse(a, pv.n_requests, p.layer, p.request, head, column, top, sum);
                     }
                 } else {
@@ -673,27 +701,28 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
             __syncthreads();
         } else {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int c = 8 * n + 2 * t + i, column = col0 + c;
-                    const float f = !whole ? unit_scale : l[n][i] == 0.f ? 0.f : unit_scale / l[n][i];
-                    if (whole) {
-                        if (column < a.columns) {
-                            T* row = out_row<T, D>(a, pv.n_requests, p.layer, p.request, head, column) + 4 * g;
-#pragma unroll
-                            for (int j = 0; j < kGroups; ++j)
-                                store4<T>(row + 32 * j, o[n][j][0][i] * f, o[n][j][0][i + 2] * f, o[n][j][1][i] * f, o[n][j][1][i + 2] * f);
-                            if (g == 0) store_lse(a, pv.n_requests, p.layer, p.request, head, column, m[n][i], l[n][i]);
-                        }
-                    } else {
-                        float* row = a.part_o + ((size_t)slot * kCols + c) * D + 4 * g;
+            for (int i = 0; i < kOwn; ++i) {
+                const int c = tile_column(i), column = col0 + c;
+                if (whole) {
+                    if (column < a.columns) {
+                        const float f = l[i] == 0.f ? 0.f : unit_scale / l[i];
+                        T* row = out_row<T, D>(a, p.layer, p.request, head, column) + 4 * g;
 #pragma unroll
                         for (int j = 0; j < kGroups; ++j)
-                            store4<float>(row + 32 * j, o[n][j][0][i] * f, o[n][j][0][i + 2] * f, o[n][j][1][i] * f, o[n][j][1][i + 2] * f);
-                        if (g == 0) a.part_ml[(size_t)slot * 2 * kCols + c] = m[n][i], a.part_ml[(size_t)slot * 2 * kCols + kCols + c] = l[n][i];
+                            if (has(j)) {
+                                const float4 y = dims(i, j, f);
+                                store4<T>(row + 32 * j, y.x, y.y, y.z, y.w);
+                            }
+                        if (first_lane) store_lse(a, pv.n_requests, p.layer, p.request, head, column, m[i], l[i]);
                     }
+                } else {
+                    float* row = a.part_o + ((size_t)slot * kCols + c) * D + 4 * g;
+#pragma unroll
+                    for (int j = 0; j < kGroups; ++j)
+                        if (has(j)) *reinterpret_cast<float4*>(row + 32 * j) = dims(i, j, unit_scale);
+                    if (first_lane) a.part_ml[(size_t)slot * 2 * kCols + c] = m[i], a.part_ml[(size_t)slot * 2 * kCols + kCols + c] = l[i];
                 }
+            }
         }
         if (begins && !whole && lane == 0 && (!together || warp == 0)) {
             const long long more = p.length - p.end();        // of the unit in later shares
@@ -746,7 +775,7 @@ kv4_merge_kernel(Kv4Args a, PagesView pv, int cols) {
                 }
             }
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            store4<T>(out_row<T, D>(a, pv.n_requests, mark.y, mark.z, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
+            store4<T>(out_row<T, D>(a, mark.y, mark.z, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
             if (d == 0) store_lse(a, pv.n_requests, mark.y, mark.z, head, column, top, sum);
         }
     }
@@ -754,8 +783,9 @@ kv4_merge_kernel(Kv4Args a, PagesView pv, int cols) {
 
 // How a call is cut: everything the host can know of it.
 struct Cut {
-    int nt;                                       // tiles of eight query columns that a warp takes
-    int tiles, columns;
+    int nt;                                       // products of eight columns that a warp takes
+    bool few;
+    int tile, tiles, columns;                     // columns of a unit, units and columns of a kv head
     int ctas, n_shares, warps_per_share;
 };
 
@@ -763,7 +793,9 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
     Cut c = {};
     c.columns = g->n_q_heads / g->n_kv_heads * q_len;
     c.nt = c.columns <= 8 ? 1 : 2;
-    c.tiles = (c.columns + 8 * c.nt - 1) / (8 * c.nt);
+    c.few = c.columns <= tile_columns(g->head_dim, 1, true);
+    c.tile = tile_columns(g->head_dim, c.nt, c.few);
+    c.tiles = (c.columns + c.tile - 1) / c.tile;
     c.ctas = sm_count() * (c.nt == 1 ? 2 : 1);
     const double units = (double)n_layers * p->n_requests * g->n_kv_heads * c.tiles;
     c.warps_per_share = units >= FACTOR * c.ctas * kWarps ? 1 : kWarps;
@@ -779,33 +811,37 @@ int check_attn(const cf_geom* geom, const cf_pages* pages, int q_len, int n_laye
     if (rc != CF_OK) return rc;
     if (q_len <= 0 || n_layers <= 0 || n_layers > 65535) return CF_ERR_INVALID_ARG;
     const long long columns = (long long)geom->n_q_heads / geom->n_kv_heads * q_len;
-    const long long tiles = (columns + 7) / 8;
+    const long long tiles = columns / 2 + 1;      // at least as many as cut_of makes
     if (columns > (1 << 24) || tiles * geom->n_kv_heads * ((long long)pages->table_cols * (pages->page_rows / 16) / kStepBlocks + 2 + kMostCost) > INT_MAX)
         return CF_ERR_INVALID_ARG;                // a request's part of the line is counted in 32 bits
     return CF_OK;
 }
 
-size_t attn_smem(int head_dim, int nt) {
-    return (size_t)kWarps * kStages * kStepBlocks * block_bytes(head_dim) + (size_t)kWarps * 8 * nt * (head_dim + 4) * 4 + 2 * (size_t)kWarps * 8 * nt * 4 +
+size_t attn_smem(int head_dim, int tile) {
+    return (size_t)kWarps * kStages * kStepBlocks * block_bytes(head_dim) + (size_t)kWarps * tile * (head_dim + 4) * 4 + 2 * (size_t)kWarps * tile * 4 +
            (size_t)kWarps * kStages * 8;
 }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool FEW>
 int launch_attn(const Kv4Args& a, const PagesView& pv, int ctas, cudaStream_t stream) {
     static PerDeviceOnce once;
-    const size_t smem = attn_smem(D, NT);
-    const int rc = configure_smem_once(once, kv4_attn_kernel<T, D, NT>, (int)smem);
+    const size_t smem = attn_smem(D, tile_columns(D, NT, FEW));
+    const int rc = configure_smem_once(once, kv4_attn_kernel<T, D, NT, FEW>, (int)smem);
     if (rc != CF_OK) return rc;
-    const int err = launch_chained(kv4_attn_kernel<T, D, NT>, dim3((unsigned)ctas), kThreads, smem, stream, a, pv);
+    const int err = launch_chained(kv4_attn_kernel<T, D, NT, FEW>, dim3((unsigned)ctas), kThreads, smem, stream, a, pv);
     if (err != CF_OK) return err;
-    return launch_chained(kv4_merge_kernel<T, D>, dim3((unsigned)a.n_shares), kMergeThreads, 0, stream, a, pv, 8 * NT);
+    return launch_chained(kv4_merge_kernel<T, D>, dim3((unsigned)a.n_shares), kMergeThreads, 0, stream, a, pv, tile_columns(D, NT, FEW));
+}
+
+template <typename T, int D>
+int launch_attn_cut(const Kv4Args& a, const PagesView& pv, const Cut& c, cudaStream_t stream) {
+    if (c.few) return launch_attn<T, D, 1, true>(a, pv, c.ctas, stream);
+    return c.nt == 1 ? launch_attn<T, D, 1, false>(a, pv, c.ctas, stream) : launch_attn<T, D, 2, false>(a, pv, c.ctas, stream);
 }
 
 template <typename T>
 int launch_attn_typed(const Kv4Args& a, const PagesView& pv, const Cut& c, int head_dim, cudaStream_t stream) {
-    if (head_dim == 128)
-        return c.nt == 1 ? launch_attn<T, 128, 1>(a, pv, c.ctas, stream) : launch_attn<T, 128, 2>(a, pv, c.ctas, stream);
-    return c.nt == 1 ? launch_attn<T, 64, 1>(a, pv, c.ctas, stream) : launch_attn<T, 64, 2>(a, pv, c.ctas, stream);
+    return head_dim == 128 ? launch_attn_cut<T, 128>(a, pv, c, stream) : launch_attn_cut<T, 64>(a, pv, c, stream);
 }
 
 }  // namespace
@@ -819,7 +855,7 @@ extern "C" {
 size_t cf_kv4_attn_workspace_bytes(const cf_geom* geom, const cf_pages* pages, int32_t q_len, int32_t n_layers) {
     if (check_attn(geom, pages, q_len, n_layers) != CF_OK) return 0;
     const Cut c = cut_of(geom, pages, q_len, n_layers);
-    const size_t rows = 2 * (size_t)c.n_shares * 8 * c.nt;
+    const size_t rows = 2 * (size_t)c.n_shares * c.tile;
     return round_up(rows * geom->head_dim * 4) + round_up(rows * 8) + round_up((size_t)c.n_shares * sizeof(int4));
 }
 
@@ -841,7 +877,7 @@ int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, in
         return CF_ERR_WORKSPACE;
     const Cut c = cut_of(geom, pages, q_len, n_layers);
     const float scale = softmax_scale != 0.f ? softmax_scale : 1.f / sqrtf((float)geom->head_dim);
-    const size_t rows = 2 * (size_t)c.n_shares * 8 * c.nt;
+    const size_t rows = 2 * (size_t)c.n_shares * c.tile;
     char* w = static_cast<char*>(workspace);
     Kv4Args a = {};
     a.q = q, a.kv4 = static_cast<const unsigned char*>(kv4), a.out = out, a.lse = lse;
