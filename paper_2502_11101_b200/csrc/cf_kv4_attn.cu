@@ -36,8 +36,6 @@ using tc::smem_u32;
 
 namespace {
 
-constexpr int kWarps = 8;
-constexpr int kThreads = 32 * kWarps;
 constexpr int kStages = 2;                        // steps of the ring
 constexpr int kStepBlocks = 2;                    // blocks of a step
 constexpr int kStepRows = kStepBlocks * kBlockRows;
@@ -46,15 +44,15 @@ constexpr float kSlack = 8.f;                     // how far a logit may lie abo
 constexpr int kHead = 7;                          // P is at most 2^kSlack * 2^kHead, below fp16's 2^16
 constexpr int kLeastExponent = -110;
 constexpr int kMostCost = 32;                     // of a unit, in steps
-#ifndef FACTOR
-#define FACTOR 2.0
-#define LEAST1 4
-#define COST1 3
-#endif
-#ifndef LEAST
-#define LEAST kWarps
-#define COST 16
-#endif
+// A share is at least this long, in steps; a unit costs this much besides its steps (its queries, the join of its parts); by
+// the warps that have a share of their own, or the CTA that has one.
+constexpr int kLeastAlone = 4, kLeastTogether = 8;
+constexpr int kCostAlone = 3, kCostTogether = 16;
+
+// Warps of a CTA, and CTAs of an SM.  With few columns the loop fits 128 registers: 16 warps per SM; without, and with twice the
+// columns, fewer warps with more registers are faster.
+__host__ __device__ constexpr int warps_of(bool few) { return few ? 8 : 4; }
+__host__ __device__ constexpr int ctas_per_sm(int nt, bool few) { return few ? 2 : nt == 1 ? 3 : 2; }
 
 // Query columns of a unit.
 __host__ __device__ constexpr int tile_columns(int head_dim, int nt, bool few) { return few ? 8 / (head_dim / 32) : 8 * nt; }
@@ -66,11 +64,12 @@ struct Kv4Args {
     float* lse;
     float* part_o;                                // [2 shares][columns][D]
     float* part_ml;                               // [2 shares][2][columns]
-    int4* marks;                                  // [shares] what a share leaves for the merge: parts, layer, request, head * tiles + tile
+    int4* marks;                                  // for the merge, by unit or by share: parts, first share, layer * requests + request, unit
     long long q_layer_stride, kv4_layer_stride, out_layer_stride;
     int n_layers, q_len, n_q_heads, n_kv_heads, columns;                   // columns = query heads of a kv head * q_len
     Divisor group, tiles, blocks_per_page;
     int n_shares, warps_per_share, unit_cost;
+    int marks_by_unit;                            // a mark for every unit, where there are fewer units than shares
     long long least_share;
     float scale_log2;
 };
@@ -289,9 +288,10 @@ __device__ __forceinline__ void store_lse(const Kv4Args& a, int n_requests, int 
 // FEW: the query columns times the groups fit the eight columns of a matrix product, which then has a column per (query, group):
 // one chain of products for all groups, and one set of probabilities instead of one per group.
 template <typename T, int D, int NT, bool FEW>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 2 : 1)
+__global__ void __launch_bounds__(32 * warps_of(FEW), ctas_per_sm(NT, FEW))
 kv4_attn_kernel(Kv4Args args, PagesView pv) {
     chain_next();
+    constexpr int kWarps = warps_of(FEW), kThreads = 32 * kWarps;
     constexpr int kBytes = block_bytes(D);
     constexpr int kRing = kStages * kStepBlocks * kBytes;    // of a warp
     constexpr int kGroups = D / 32;
@@ -325,7 +325,8 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
     const long long per_layer = line.length_of_layer(), total = per_layer * a.n_layers;
     const long long size = max(a.least_share, (total + a.n_shares - 1) / a.n_shares);
     const long long begin = share * size, mine = min(size, total - begin);
-    if (lane == 0 && (!together || warp == 0)) a.marks[share] = make_int4(0, 0, 0, 0);
+    const bool writer = lane == 0 && (!together || warp == 0);
+    if (writer && !a.marks_by_unit) a.marks[share] = make_int4(0, 0, 0, 0);
     if (share == 0 && (!together || warp == 0))
         for (int b = lane; b < pv.n_requests; b += 32)
             if (pv.rows[b] < 0 || pv.rows[b] > line.most) atomicCAS(pv.status, 0, CF_ERR_RANGE);
@@ -724,9 +725,10 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                 }
             }
         }
-        if (begins && !whole && lane == 0 && (!together || warp == 0)) {
+        if (writer && begins && (!whole || a.marks_by_unit)) {
             const long long more = p.length - p.end();        // of the unit in later shares
-            a.marks[share] = make_int4(1 + (int)((more + size - 1) / size), p.layer, p.request, p.unit);
+            const int lb = p.layer * pv.n_requests + p.request;
+            a.marks[a.marks_by_unit ? lb * line.units + p.unit : share] = make_int4(whole ? 0 : 1 + (int)((more + size - 1) / size), share, lb, p.unit);
         }
     }
     if (given_up) {                                          // its copies in flight are given the time to end
@@ -738,45 +740,64 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
     }
 }
 
-constexpr int kAtOnce = 4;
+// A part of a column's dims, or the sum of several.
+struct Part {
+    float top, sum;
+    float4 x;
+    __device__ __forceinline__ void add(float m, float l, const float4& y) {
+        if (m == -INFINITY && l == 0.f) return;              // no key seen
+        const float to = fmaxf(top, m), f0 = top == to ? 1.f : exp2f(top - to), f1 = m == to || m == -INFINITY ? 1.f : exp2f(m - to);
+        sum = fmaf(sum, f0, l * f1);
+        x.x = fmaf(x.x, f0, y.x * f1), x.y = fmaf(x.y, f0, y.y * f1), x.z = fmaf(x.z, f0, y.z * f1), x.w = fmaf(x.w, f0, y.w * f1);
+        top = to;
+    }
+};
 
-// Joins the parts of the unit that begins in share blockIdx.x and goes on in later ones.
+constexpr int kAtOnce = 4;                        // parts whose loads are under way together
+
+// Joins the parts of the units that were cut: a block per mark and `cols` of the unit's columns, whose threads have a column's
+// four dims each and, where that leaves some, every n-th part.  Joining a unit of a hundred parts in one block took 12 us (a
+// request of 24 000 rows, 28/4 heads: 31 us a call).
 template <typename T, int D>
 __global__ void __launch_bounds__(kMergeThreads)
-kv4_merge_kernel(Kv4Args a, PagesView pv, int cols) {
+kv4_merge_kernel(Kv4Args args, PagesView pv, Divisor requests, int tile, int cols, int lanes_log2) {
     chain_next();
+    __shared__ Part s_part[kMergeThreads];
     chain_wait();
-    const int share = blockIdx.x;
-    const int4 mark = a.marks[share];
+    const Kv4Args& a = args;
+    const int4 mark = a.marks[blockIdx.x];
     if (mark.x > 0) {
-        const int head = a.tiles.quotient(mark.w), col0 = (mark.w - head * (int)a.tiles.d) * cols;
-        for (int i = threadIdx.x; i < cols * (D / 4); i += kMergeThreads) {
-            const int c = i / (D / 4), d = i % (D / 4) * 4, column = col0 + c;
-            if (column >= a.columns) continue;
-            float top = -INFINITY, sum = 0.f;
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int k0 = 0; k0 < mark.x; k0 += kAtOnce) {    // that many parts' loads are under way together
-                float m[kAtOnce], l[kAtOnce];
-                float4 y[kAtOnce];
+        const int lanes = 1 << lanes_log2, n = kMergeThreads >> lanes_log2;       // a column's dims have D/4 lanes
+        const int k0 = threadIdx.x >> lanes_log2, i = threadIdx.x & (lanes - 1), c = blockIdx.y * cols + i / (D / 4), d = i % (D / 4) * 4;
+        const int head = a.tiles.quotient(mark.w), column = (mark.w - head * (int)a.tiles.d) * tile + c;
+        Part x = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+        for (int k = k0; k < mark.x; k += n * kAtOnce) {
+            float m[kAtOnce], l[kAtOnce];
+            float4 y[kAtOnce];
 #pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    const int part = min(k0 + k, mark.x - 1);
-                    const size_t slot = part == 0 ? 2 * (size_t)share + 1 : 2 * (size_t)(share + part);
-                    m[k] = a.part_ml[slot * 2 * cols + c], l[k] = a.part_ml[slot * 2 * cols + cols + c];
-                    y[k] = *reinterpret_cast<const float4*>(a.part_o + (slot * cols + c) * D + d);
-                }
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    if (k0 + k >= mark.x || (m[k] == -INFINITY && l[k] == 0.f)) continue;
-                    const float to = fmaxf(top, m[k]), f0 = top == to ? 1.f : exp2f(top - to), f1 = m[k] == to || m[k] == -INFINITY ? 1.f : exp2f(m[k] - to);
-                    sum = fmaf(sum, f0, l[k] * f1);
-                    x.x = fmaf(x.x, f0, y[k].x * f1), x.y = fmaf(x.y, f0, y[k].y * f1), x.z = fmaf(x.z, f0, y[k].z * f1), x.w = fmaf(x.w, f0, y[k].w * f1);
-                    top = to;
-                }
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int part = min(k + j * n, mark.x - 1);
+                const size_t slot = part == 0 ? 2 * (size_t)mark.y + 1 : 2 * (size_t)(mark.y + part);
+                m[j] = a.part_ml[slot * 2 * tile + c], l[j] = a.part_ml[slot * 2 * tile + tile + c];
+                y[j] = *reinterpret_cast<const float4*>(a.part_o + (slot * tile + c) * D + d);
             }
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            store4<T>(out_row<T, D>(a, mark.y, mark.z, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
-            if (d == 0) store_lse(a, pv.n_requests, mark.y, mark.z, head, column, top, sum);
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j)
+                if (k + j * n < mark.x) x.add(m[j], l[j], y[j]);
+        }
+        if (n > 1) {
+            s_part[threadIdx.x] = x;
+            __syncthreads();
+        }
+        if (k0 == 0 && column < a.columns) {
+            for (int k = 1; k < n; ++k) {
+                const Part& y = s_part[k * lanes + i];
+                x.add(y.top, y.sum, y.x);
+            }
+            const int layer = requests.quotient(mark.z), request = mark.z - layer * pv.n_requests;
+            const float inv = x.sum == 0.f ? 0.f : 1.f / x.sum;
+            store4<T>(out_row<T, D>(a, layer, request, head, column) + d, x.x.x * inv, x.x.y * inv, x.x.z * inv, x.x.w * inv);
+            if (d == 0) store_lse(a, pv.n_requests, layer, request, head, column, x.top, x.sum);
         }
     }
 }
@@ -786,7 +807,9 @@ struct Cut {
     int nt;                                       // products of eight columns that a warp takes
     bool few;
     int tile, tiles, columns;                     // columns of a unit, units and columns of a kv head
-    int ctas, n_shares, warps_per_share;
+    int warps, ctas, n_shares, warps_per_share;
+    int marks;                                    // units, or shares where they are fewer
+    bool marks_by_unit;
 };
 
 Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
@@ -796,10 +819,17 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
     c.few = c.columns <= tile_columns(g->head_dim, 1, true);
     c.tile = tile_columns(g->head_dim, c.nt, c.few);
     c.tiles = (c.columns + c.tile - 1) / c.tile;
-    c.ctas = sm_count() * (c.nt == 1 ? 2 : 1);
+    c.warps = warps_of(c.few);
+    c.ctas = sm_count() * ctas_per_sm(c.nt, c.few);
+    // A CTA's warps pay for every unit of a share of theirs with a barrier and a join, about 16 steps of the line; warps with shares
+    // of their own with 3 steps for every unit and every share.  With U units and W warps: 16 U against 3 (U + W).
+    // Measured (together / alone, us): 96 requests, 28/4 (U = 0.22 W) 46.7 / 44.9; 512 short ones, 32/8 (2.3 W) 94.6 / 39.4;
+    // 3 requests, four layers, 32/8 (0.05 W) 17.3 / 21.2; 8 long ones, 32/32 (0.11 W) 122 / 126.
     const double units = (double)n_layers * p->n_requests * g->n_kv_heads * c.tiles;
-    c.warps_per_share = units >= FACTOR * c.ctas * kWarps ? 1 : kWarps;
-    c.n_shares = c.warps_per_share == 1 ? c.ctas * kWarps : c.ctas;
+    c.warps_per_share = 5.0 * units >= (double)c.ctas * c.warps ? 1 : c.warps;
+    c.n_shares = c.warps_per_share == 1 ? c.ctas * c.warps : c.ctas;
+    c.marks_by_unit = units <= c.n_shares;
+    c.marks = c.marks_by_unit ? (int)units : c.n_shares;
     return c;
 }
 
@@ -811,32 +841,40 @@ int check_attn(const cf_geom* geom, const cf_pages* pages, int q_len, int n_laye
     if (rc != CF_OK) return rc;
     if (q_len <= 0 || n_layers <= 0 || n_layers > 65535) return CF_ERR_INVALID_ARG;
     const long long columns = (long long)geom->n_q_heads / geom->n_kv_heads * q_len;
+    if ((long long)n_layers * pages->n_requests > INT_MAX) return CF_ERR_INVALID_ARG;
     const long long tiles = columns / 2 + 1;      // at least as many as cut_of makes
     if (columns > (1 << 24) || tiles * geom->n_kv_heads * ((long long)pages->table_cols * (pages->page_rows / 16) / kStepBlocks + 2 + kMostCost) > INT_MAX)
         return CF_ERR_INVALID_ARG;                // a request's part of the line is counted in 32 bits
     return CF_OK;
 }
 
-size_t attn_smem(int head_dim, int tile) {
-    return (size_t)kWarps * kStages * kStepBlocks * block_bytes(head_dim) + (size_t)kWarps * tile * (head_dim + 4) * 4 + 2 * (size_t)kWarps * tile * 4 +
-           (size_t)kWarps * kStages * 8;
+size_t attn_smem(int head_dim, int warps, int tile) {
+    return (size_t)warps * kStages * kStepBlocks * block_bytes(head_dim) + (size_t)warps * tile * (head_dim + 4) * 4 + 2 * (size_t)warps * tile * 4 +
+           (size_t)warps * kStages * 8;
 }
 
 template <typename T, int D, int NT, bool FEW>
-int launch_attn(const Kv4Args& a, const PagesView& pv, int ctas, cudaStream_t stream) {
+int launch_attn(const Kv4Args& a, const PagesView& pv, int ctas, int marks, cudaStream_t stream) {
     static PerDeviceOnce once;
-    const size_t smem = attn_smem(D, tile_columns(D, NT, FEW));
+    const size_t smem = attn_smem(D, warps_of(FEW), tile_columns(D, NT, FEW));
     const int rc = configure_smem_once(once, kv4_attn_kernel<T, D, NT, FEW>, (int)smem);
     if (rc != CF_OK) return rc;
-    const int err = launch_chained(kv4_attn_kernel<T, D, NT, FEW>, dim3((unsigned)ctas), kThreads, smem, stream, a, pv);
+    const int err = launch_chained(kv4_attn_kernel<T, D, NT, FEW>, dim3((unsigned)ctas), 32 * warps_of(FEW), smem, stream, a, pv);
     if (err != CF_OK) return err;
-    return launch_chained(kv4_merge_kernel<T, D>, dim3((unsigned)a.n_shares), kMergeThreads, 0, stream, a, pv, tile_columns(D, NT, FEW));
+    // a block takes all columns of a unit where units are many, fewer where they are not
+    constexpr int tile = tile_columns(D, NT, FEW);
+    int cols = std::min(tile, kMergeThreads / (D / 4));
+    while (cols > 1 && marks * (tile / cols) < 2 * sm_count()) cols /= 2;
+    int lanes_log2 = 0;
+    while (1 << lanes_log2 < cols * (D / 4)) ++lanes_log2;
+    return launch_chained(kv4_merge_kernel<T, D>, dim3((unsigned)marks, (unsigned)(tile / cols)), kMergeThreads, 0, stream, a, pv,
+                          Divisor(pv.n_requests), tile, cols, lanes_log2);
 }
 
 template <typename T, int D>
 int launch_attn_cut(const Kv4Args& a, const PagesView& pv, const Cut& c, cudaStream_t stream) {
-    if (c.few) return launch_attn<T, D, 1, true>(a, pv, c.ctas, stream);
-    return c.nt == 1 ? launch_attn<T, D, 1, false>(a, pv, c.ctas, stream) : launch_attn<T, D, 2, false>(a, pv, c.ctas, stream);
+    if (c.few) return launch_attn<T, D, 1, true>(a, pv, c.ctas, c.marks, stream);
+    return c.nt == 1 ? launch_attn<T, D, 1, false>(a, pv, c.ctas, c.marks, stream) : launch_attn<T, D, 2, false>(a, pv, c.ctas, c.marks, stream);
 }
 
 template <typename T>
@@ -856,7 +894,7 @@ size_t cf_kv4_attn_workspace_bytes(const cf_geom* geom, const cf_pages* pages, i
     if (check_attn(geom, pages, q_len, n_layers) != CF_OK) return 0;
     const Cut c = cut_of(geom, pages, q_len, n_layers);
     const size_t rows = 2 * (size_t)c.n_shares * c.tile;
-    return round_up(rows * geom->head_dim * 4) + round_up(rows * 8) + round_up((size_t)c.n_shares * sizeof(int4));
+    return round_up(rows * geom->head_dim * 4) + round_up(rows * 8) + round_up((size_t)c.marks * sizeof(int4));
 }
 
 int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q,
@@ -888,9 +926,9 @@ int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, in
     a.n_layers = n_layers, a.q_len = q_len, a.n_q_heads = geom->n_q_heads, a.n_kv_heads = geom->n_kv_heads;
     a.columns = c.columns;
     a.group = Divisor(geom->n_q_heads / geom->n_kv_heads), a.tiles = Divisor(c.tiles), a.blocks_per_page = Divisor(pages->page_rows / kBlockRows);
-    a.n_shares = c.n_shares, a.warps_per_share = c.warps_per_share;
-    a.least_share = c.warps_per_share == 1 ? LEAST1 : LEAST;
-    a.unit_cost = c.warps_per_share == 1 ? COST1 : COST;
+    a.n_shares = c.n_shares, a.warps_per_share = c.warps_per_share, a.marks_by_unit = c.marks_by_unit;
+    a.least_share = c.warps_per_share == 1 ? kLeastAlone : kLeastTogether;
+    a.unit_cost = c.warps_per_share == 1 ? kCostAlone : kCostTogether;
     a.scale_log2 = scale * kLog2e;
     const PagesView pv = make_pages_view(pages);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
