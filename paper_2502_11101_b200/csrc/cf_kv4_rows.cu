@@ -15,72 +15,101 @@ namespace {
 constexpr int kRowThreads = 256;
 constexpr int kRowsPerWarp = 4;
 
-// Four consecutive numbers as fp32.
-template <typename T> __device__ __forceinline__ void load4(const T* p, float (&x)[4]);
-template <> __device__ __forceinline__ void load4<float>(const float* p, float (&x)[4]) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-}
-template <> __device__ __forceinline__ void load4<__nv_bfloat16>(const __nv_bfloat16* p, float (&x)[4]) {
-    const uint2 v = *reinterpret_cast<const uint2*>(p);
-    x[0] = bf16_low(v.x), x[1] = bf16_high(v.x), x[2] = bf16_low(v.y), x[3] = bf16_high(v.y);
-}
-template <typename T> __device__ __forceinline__ void store4(T* p, const float (&x)[4]);
-template <> __device__ __forceinline__ void store4<float>(float* p, const float (&x)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-}
-template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, const float (&x)[4]) {
+__device__ __forceinline__ void store4(float* p, const float (&x)[4]) { *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, const float (&x)[4]) {
     const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
     *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
 
-// The scale of a group whose largest magnitude has these bits: bf16 bits, and whether codes other than 0 are kept.
-__device__ __forceinline__ uint32_t scale_of(uint32_t amax, float& scale) {
-    scale = 0.f;
-    if (amax >= 0x7f800000u) return 0x7fffu;                       // not finite
-    // one rounding: a quotient by 6 of 24 bits that is not a tie between bf16 numbers is no nearer to one than its rounding
-    const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__uint_as_float(amax), 6.f)));
-    if (s < 1.1754944e-38f) return 0u;
-    scale = s;
-    return __float_as_uint(s) >> 16;
-}
+// A lane's four numbers of each group.  amax: the largest magnitude's upper 16 bits of groups 2i and 2i + 1, magnitudes
+// ordering as integers with everything that is not finite on top; scale, codes: what a group is kept as.
+template <typename T, int D> struct Numbers;
 
-// Codes of a lane's four numbers of a group, 16 bits.
-__device__ __forceinline__ uint32_t codes4(const float (&x)[4], float scale) {
-    if (scale == 0.f) return 0u;
-    return two_codes(__fdiv_rn(x[0], scale), __fdiv_rn(x[1], scale)) | two_codes(__fdiv_rn(x[2], scale), __fdiv_rn(x[3], scale)) << 8;
-}
+// bf16.  Quotients are needed only to tell on which side of the border between two codes they lie, and numbers of eight bits
+// leave no close calls.  x / s lies on a border m / 4 (m = 1, 3, 5, 7, 10, 14, 20) exactly, or at least 2^-11 off it: x - s m / 4
+// is a multiple of the smaller of x's last place and a quarter of s's, and x / s > 0.2 bounds the ratio of the two.  So x times
+// an approximate 1 / s, rounded to multiples of 2^-16 (what adding 192 does), is on the border when x / s is and on the right
+// side otherwise.  In the same way amax / 6 is never within 2^-11 of its size of a border between two bf16 numbers, and a
+// product with 1 / 6 will do.
+template <int D> struct Numbers<__nv_bfloat16, D> {
+    uint2 w[D / 32];
+    __device__ __forceinline__ void load(const __nv_bfloat16* row, int u) {
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) w[j] = *reinterpret_cast<const uint2*>(row + 32 * j + 4 * u);
+    }
+    __device__ __forceinline__ void scales_of(uint32_t (&scales)[D / 64]) const {
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            constexpr uint32_t kMagnitude = 0x7fff7fffu;
+            const uint32_t a = __vmaxu2(w[2 * i].x & kMagnitude, w[2 * i].y & kMagnitude), b = __vmaxu2(w[2 * i + 1].x & kMagnitude, w[2 * i + 1].y & kMagnitude);
+            uint32_t amax = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));   // of both groups
+#pragma unroll
+            for (int o = 1; o < 8; o <<= 1) amax = __vmaxu2(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            const __nv_bfloat162 s = __floats2bfloat162_rn(bf16_low(amax) * (1.f / 6.f), bf16_high(amax) * (1.f / 6.f));
+            uint32_t lo = *reinterpret_cast<const uint32_t*>(&s) & 0xffffu, hi = *reinterpret_cast<const uint32_t*>(&s) >> 16;
+            if (lo < 0x0080u) lo = 0u;                       // below 2^-126
+            if (hi < 0x0080u) hi = 0u;
+            if ((amax & 0xffffu) >= 0x7f80u) lo = 0x7fffu;
+            if (amax >= 0x7f800000u) hi = 0x7fffu;
+            scales[i] = lo | hi << 16;
+        }
+    }
+    __device__ __forceinline__ uint32_t codes_of(int j, uint32_t scale_bits) const {
+        const float s = __uint_as_float(scale_bits << 16);
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+        auto quotient = [&](float x) {                       // with the sign of x also where it rounds to zero
+            return __uint_as_float(__float_as_uint(fmaf(x, r, 192.f) - 192.f) | (__float_as_uint(x) & 0x80000000u));
+        };
+        const uint32_t codes = two_codes(quotient(bf16_low(w[j].x)), quotient(bf16_high(w[j].x))) |
+                               two_codes(quotient(bf16_low(w[j].y)), quotient(bf16_high(w[j].y))) << 8;
+        return scale_bits == 0u || scale_bits == 0x7fffu ? 0u : codes;
+    }
+};
 
-// A lane's dims of one row (of keys or values): codes of group j in 16 bits of `codes`, all groups' scales in `scales`.
+// fp32: divisions.  A quotient rounded to 24 bits is on a border (of three bits, of nine for the scale) only if the exact one
+// is: the dividend's last place is more than half of the border's.
+template <int D> struct Numbers<float, D> {
+    float4 w[D / 32];
+    __device__ __forceinline__ void load(const float* row, int u) {
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) w[j] = *reinterpret_cast<const float4*>(row + 32 * j + 4 * u);
+    }
+    __device__ __forceinline__ static uint32_t scale_of(uint32_t amax) {
+        if (amax >= 0x7f800000u) return 0x7fffu;
+        const float s = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(__uint_as_float(amax), 6.f)));
+        return s < 1.1754944e-38f ? 0u : __float_as_uint(s) >> 16;
+    }
+    __device__ __forceinline__ void scales_of(uint32_t (&scales)[D / 64]) const {
+        uint32_t amax[D / 32];
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+            constexpr uint32_t kMagnitude = 0x7fffffffu;
+            amax[j] = max(max(__float_as_uint(w[j].x) & kMagnitude, __float_as_uint(w[j].y) & kMagnitude),
+                          max(__float_as_uint(w[j].z) & kMagnitude, __float_as_uint(w[j].w) & kMagnitude));
+        }
+#pragma unroll
+        for (int o = 1; o < 8; o <<= 1)
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) amax[j] = max(amax[j], __shfl_xor_sync(0xffffffffu, amax[j], o));
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) scales[i] = scale_of(amax[2 * i]) | scale_of(amax[2 * i + 1]) << 16;
+    }
+    __device__ __forceinline__ uint32_t codes_of(int j, uint32_t scale_bits) const {
+        if (scale_bits == 0u || scale_bits == 0x7fffu) return 0u;
+        const float s = __uint_as_float(scale_bits << 16);
+        return two_codes(__fdiv_rn(w[j].x, s), __fdiv_rn(w[j].y, s)) | two_codes(__fdiv_rn(w[j].z, s), __fdiv_rn(w[j].w, s)) << 8;
+    }
+};
+
+// A lane's dims of one row: codes of groups 2i and 2i + 1 in the halves of codes[i], the scales likewise.
 template <typename T, int D>
-__device__ __forceinline__ void quantise(const T* row, int u, uint32_t (&codes)[D / 64], uint32_t (&scales)[D / 64]) {
-    float x[D / 32][4];
-    uint32_t amax[D / 32];
+__device__ __forceinline__ void quantise(const Numbers<T, D>& x, uint32_t (&codes)[D / 64], uint32_t (&scales)[D / 64]) {
+    x.scales_of(scales);
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) load4<T>(row + 32 * j + 4 * u, x[j]);
-#pragma unroll
-    for (int j = 0; j < D / 32; ++j) {
-        uint32_t a = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a = max(a, __float_as_uint(x[j][i]) & 0x7fffffffu);     // magnitudes order as integers, NaN on top
-        amax[j] = a;
-    }
-#pragma unroll
-    for (int o = 1; o < 8; o <<= 1)
-#pragma unroll
-        for (int j = 0; j < D / 32; ++j) amax[j] = max(amax[j], __shfl_xor_sync(0xffffffffu, amax[j], o));
-#pragma unroll
-    for (int j = 0; j < D / 32; j += 2) {
-        float s0, s1;
-        scales[j / 2] = scale_of(amax[j], s0);
-        scales[j / 2] |= scale_of(amax[j + 1], s1) << 16;
-        codes[j / 2] = codes4(x[j], s0) | codes4(x[j + 1], s1) << 16;
-    }
+    for (int i = 0; i < D / 64; ++i) codes[i] = x.codes_of(2 * i, scales[i] & 0xffffu) | x.codes_of(2 * i + 1, scales[i] >> 16) << 16;
 }
 
-template <int N> struct Words;
-template <> struct Words<1> { using type = uint32_t; };
-template <> struct Words<2> { using type = uint2; };
 template <int N> __device__ __forceinline__ void store_words(unsigned char* p, const uint32_t (&w)[N]) {
     if (N == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[N - 1]);
     else *reinterpret_cast<uint32_t*>(p) = w[0];
@@ -129,7 +158,7 @@ __device__ __forceinline__ void dequantise(const uint32_t (&codes)[D / 64], cons
         const float s = j & 1 ? bf16_high(scales[j / 2]) : bf16_low(scales[j / 2]);
         const float2 fa = __half22float2(*reinterpret_cast<const __half2*>(&a)), fb = __half22float2(*reinterpret_cast<const __half2*>(&b));
         const float x[4] = {fa.x * s, fa.y * s, fb.x * s, fb.y * s};
-        store4<T>(row + 32 * j + 4 * u, x);
+        store4(row + 32 * j + 4 * u, x);
     }
 }
 
@@ -175,13 +204,16 @@ rows_kernel(RowArgs a, Divisor page_rows, Divisor heads, Divisor quads, T* k, T*
     const size_t src = (size_t)layer * a.kv_layer_stride + (size_t)(valid ? row : quad * kRowsPerWarp) * a.row_stride + head * D;
     uint32_t codes[D / 64], scales[D / 64], words[D / 64];
     if (WRITE) {
-        quantise<T, D>(k + src, u, codes, scales);
+        Numbers<T, D> nk, nv;
+        nk.load(k + src, u);
+        nv.load(v + src, u);
+        quantise<T, D>(nk, codes, scales);
         to_key_words<D>(u, codes, words);
         if (valid) {
             store_words<D / 64>(block + key_code_at<D>(r) + (u >> 1) * (D / 8) + (u & 1) * (D / 16), words);
             if (u == 0) store_words<D / 64>(block + key_scale_at<D>(r), scales);
         }
-        quantise<T, D>(v + src, u, codes, scales);
+        quantise<T, D>(nv, codes, scales);
         if (valid) {
             store_words<D / 64>(block + value_code_at<D>(r, u), codes);
             if (u == 0) store_words<D / 64>(block + value_scale_at<D>(r), scales);
