@@ -4,6 +4,8 @@
 // row of a kv head: lane u holds dims 4u .. 4u+3 of every group of 32, which are the bytes of its own value codes (8 bytes that
 // lie together in the block) and half of a key word, so that one exchange with its neighbour gives each of the two 8 bytes
 // of key codes to store.  A warp has four rows: together they write whole 32-byte sectors of value codes.
+#include <algorithm>
+
 #include "cf_kv4.cuh"
 
 namespace cf {
@@ -37,33 +39,48 @@ template <int D> struct Numbers<__nv_bfloat16, D> {
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) w[j] = *reinterpret_cast<const uint2*>(row + 32 * j + 4 * u);
     }
+    // The larger magnitude of each half, a NaN where there is one; its sign means nothing.
+    __device__ __forceinline__ static uint32_t larger(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
     __device__ __forceinline__ void scales_of(uint32_t (&scales)[D / 64]) const {
+        uint32_t amax[D / 64], least = 0xffffffffu, most = 0u;
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) {
-            constexpr uint32_t kMagnitude = 0x7fff7fffu;
-            const uint32_t a = __vmaxu2(w[2 * i].x & kMagnitude, w[2 * i].y & kMagnitude), b = __vmaxu2(w[2 * i + 1].x & kMagnitude, w[2 * i + 1].y & kMagnitude);
-            uint32_t amax = __vmaxu2(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));   // of both groups
+            const uint32_t a = larger(w[2 * i].x, w[2 * i].y), b = larger(w[2 * i + 1].x, w[2 * i + 1].y);
+            uint32_t m = larger(__byte_perm(a, b, 0x5410), __byte_perm(a, b, 0x7632));        // of both groups
 #pragma unroll
-            for (int o = 1; o < 8; o <<= 1) amax = __vmaxu2(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-            const __nv_bfloat162 s = __floats2bfloat162_rn(bf16_low(amax) * (1.f / 6.f), bf16_high(amax) * (1.f / 6.f));
-            uint32_t lo = *reinterpret_cast<const uint32_t*>(&s) & 0xffffu, hi = *reinterpret_cast<const uint32_t*>(&s) >> 16;
-            if (lo < 0x0080u) lo = 0u;                       // below 2^-126
-            if (hi < 0x0080u) hi = 0u;
-            if ((amax & 0xffffu) >= 0x7f80u) lo = 0x7fffu;
-            if (amax >= 0x7f800000u) hi = 0x7fffu;
-            scales[i] = lo | hi << 16;
+            for (int o = 1; o < 8; o <<= 1) m = larger(m, __shfl_xor_sync(0xffffffffu, m, o));
+            amax[i] = m & 0x7fff7fffu;
+            const __nv_bfloat162 s = __floats2bfloat162_rn(bf16_low(amax[i]) * (1.f / 6.f), bf16_high(amax[i]) * (1.f / 6.f));
+            scales[i] = *reinterpret_cast<const uint32_t*>(&s);
+            least = __vminu2(least, amax[i]), most = __vmaxu2(most, amax[i]);
+        }
+        // scales that are not numbers above 2^-126, rare: looked at one by one
+        if (__any_sync(0xffffffffu, __vminu2(least, 0x02000200u) != 0x02000200u || __vmaxu2(most, 0x7f7f7f7fu) != 0x7f7f7f7fu)) {
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) {
+                uint32_t lo = scales[i] & 0xffffu, hi = scales[i] >> 16;
+                if (lo < 0x0080u) lo = 0u;
+                if (hi < 0x0080u) hi = 0u;
+                if ((amax[i] & 0xffffu) >= 0x7f80u) lo = 0x7fffu;
+                if (amax[i] >= 0x7f800000u) hi = 0x7fffu;
+                scales[i] = lo | hi << 16;
+            }
         }
     }
-    __device__ __forceinline__ uint32_t codes_of(int j, uint32_t scale_bits) const {
-        const float s = __uint_as_float(scale_bits << 16);
+    __device__ __forceinline__ uint32_t codes_of(int j, float s) const {
         float r;
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));
+        // of a group without numbers: zeros (a scale of 0 gives infinity here, a NaN itself)
         auto quotient = [&](float x) {                       // with the sign of x also where it rounds to zero
             return __uint_as_float(__float_as_uint(fmaf(x, r, 192.f) - 192.f) | (__float_as_uint(x) & 0x80000000u));
         };
         const uint32_t codes = two_codes(quotient(bf16_low(w[j].x)), quotient(bf16_high(w[j].x))) |
                                two_codes(quotient(bf16_low(w[j].y)), quotient(bf16_high(w[j].y))) << 8;
-        return scale_bits == 0u || scale_bits == 0x7fffu ? 0u : codes;
+        return r < INFINITY ? codes : 0u;
     }
 };
 
@@ -95,9 +112,8 @@ template <int D> struct Numbers<float, D> {
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) scales[i] = scale_of(amax[2 * i]) | scale_of(amax[2 * i + 1]) << 16;
     }
-    __device__ __forceinline__ uint32_t codes_of(int j, uint32_t scale_bits) const {
-        if (scale_bits == 0u || scale_bits == 0x7fffu) return 0u;
-        const float s = __uint_as_float(scale_bits << 16);
+    __device__ __forceinline__ uint32_t codes_of(int j, float s) const {
+        if (!(s > 0.f)) return 0u;
         return two_codes(__fdiv_rn(w[j].x, s), __fdiv_rn(w[j].y, s)) | two_codes(__fdiv_rn(w[j].z, s), __fdiv_rn(w[j].w, s)) << 8;
     }
 };
@@ -107,7 +123,7 @@ template <typename T, int D>
 __device__ __forceinline__ void quantise(const Numbers<T, D>& x, uint32_t (&codes)[D / 64], uint32_t (&scales)[D / 64]) {
     x.scales_of(scales);
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) codes[i] = x.codes_of(2 * i, scales[i] & 0xffffu) | x.codes_of(2 * i + 1, scales[i] >> 16) << 16;
+    for (int i = 0; i < D / 64; ++i) codes[i] = x.codes_of(2 * i, bf16_low(scales[i])) | x.codes_of(2 * i + 1, bf16_high(scales[i])) << 16;
 }
 
 template <int N> __device__ __forceinline__ void store_words(unsigned char* p, const uint32_t (&w)[N]) {
@@ -169,74 +185,83 @@ struct RowArgs {
     int* status;
 };
 
-// Where a slot's row lies: the block, and the row in it; false for a row that goes nowhere.
-__device__ __forceinline__ bool find_row(const RowArgs& a, Divisor page_rows, int row, int head, int block_size, size_t& at, int& r, bool report) {
-    const long long slot = row < a.n_rows ? a.slots[row] : -1;
-    if (slot < 0) return false;
-    if (slot >= a.n_slots) {
-        if (report) atomicCAS(a.status, 0, CF_ERR_RANGE);
-        return false;
-    }
-    const long long page = slot < 0x7fffffffLL - a.page_rows ? page_rows.quotient((int)slot) : slot / a.page_rows;
-    const int in_page = (int)(slot - page * a.page_rows);
-    at = ((size_t)(page * a.n_kv_heads + head) * (a.page_rows / kBlockRows) + in_page / kBlockRows) * block_size;
-    r = in_page % kBlockRows;
-    return true;
-}
-
-// WRITE: rows to slots; otherwise slots to rows.
+// WRITE: rows to slots; otherwise slots to rows.  A warp takes four rows of `run` heads, one after the other.
 template <typename T, int D, bool WRITE>
 __global__ void __launch_bounds__(kRowThreads)
-rows_kernel(RowArgs a, Divisor page_rows, Divisor heads, Divisor quads, T* k, T* v, unsigned char* kv4) {
+rows_kernel(RowArgs args, Divisor page_rows, Divisor runs, Divisor quads, int run, T* k, T* v, unsigned char* kv4) {
     chain_next();
     chain_wait();
+    const RowArgs& a = args;
     const int lane = threadIdx.x & 31, u = lane & 7;
-    const int item = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);      // (layer, four rows, head)
-    const int rest = heads.quotient(item), head = item - rest * a.n_kv_heads;
+    const int item = blockIdx.x * (kRowThreads / 32) + (threadIdx.x >> 5);      // (layer, four rows, run of heads)
+    const int rest = runs.quotient(item), first = (item - rest * (int)runs.d) * run;
     const int layer = quads.quotient(rest), quad = rest - layer * (int)quads.d;
     if (layer >= a.n_layers) return;                                            // whole warps
     const int row = quad * kRowsPerWarp + (lane >> 3);
-    size_t at = 0;
-    int r = 0;
-    const bool valid = find_row(a, page_rows, row, head, block_bytes(D), at, r, layer == 0 && head == 0 && u == 0);
+    const long long slot = row < a.n_rows ? a.slots[row] : -1;
+    const bool valid = slot >= 0 && slot < a.n_slots;
+    if (slot >= a.n_slots && layer == 0 && first == 0 && u == 0) atomicCAS(a.status, 0, CF_ERR_RANGE);
     if (__all_sync(0xffffffffu, !valid)) return;
-    unsigned char* block = kv4 + (size_t)layer * a.kv4_layer_stride + at;
-    const size_t src = (size_t)layer * a.kv_layer_stride + (size_t)(valid ? row : quad * kRowsPerWarp) * a.row_stride + head * D;
-    uint32_t codes[D / 64], scales[D / 64], words[D / 64];
-    if (WRITE) {
-        Numbers<T, D> nk, nv;
-        nk.load(k + src, u);
-        nv.load(v + src, u);
-        quantise<T, D>(nk, codes, scales);
-        to_key_words<D>(u, codes, words);
-        if (valid) {
-            store_words<D / 64>(block + key_code_at<D>(r) + (u >> 1) * (D / 8) + (u & 1) * (D / 16), words);
-            if (u == 0) store_words<D / 64>(block + key_scale_at<D>(r), scales);
+    size_t at = (size_t)layer * a.kv4_layer_stride;
+    int r = 0;
+    constexpr int kUnroll = WRITE ? 1 : 2;
+    const int per_page = a.page_rows / kBlockRows;
+    if (valid) {
+        const long long page = slot < 0x7fffffffLL - a.page_rows ? page_rows.quotient((int)slot) : slot / a.page_rows;
+        const int in_page = (int)(slot - page * a.page_rows);
+        r = in_page % kBlockRows;
+        at += ((size_t)(page * a.n_kv_heads + first) * per_page + in_page / kBlockRows) * block_bytes(D);
+    }
+    unsigned char* block = kv4 + at;
+    size_t src = (size_t)layer * a.kv_layer_stride + (size_t)(valid ? row : quad * kRowsPerWarp) * a.row_stride + first * D;
+    const int n = min(run, a.n_kv_heads - first);
+    const int key_code = key_code_at<D>(r) + (u >> 1) * (D / 8) + (u & 1) * (D / 16), value_code = value_code_at<D>(r, u);
+#pragma unroll kUnroll
+    for (int i = 0; i < n; ++i, block += (size_t)per_page * block_bytes(D), src += D) {
+        uint32_t codes[D / 64], scales[D / 64], words[D / 64];
+        if (WRITE) {
+            Numbers<T, D> nk, nv;
+            nk.load(k + src, u);
+            nv.load(v + src, u);
+            quantise<T, D>(nk, codes, scales);
+            to_key_words<D>(u, codes, words);
+            if (valid) {
+                store_words<D / 64>(block + key_code, words);
+                if (u == 0) store_words<D / 64>(block + key_scale_at<D>(r), scales);
+            }
+            quantise<T, D>(nv, codes, scales);
+            if (valid) {
+                store_words<D / 64>(block + value_code, codes);
+                if (u == 0) store_words<D / 64>(block + value_scale_at<D>(r), scales);
+            }
+        } else {
+            uint32_t value_codes[D / 64], value_scales[D / 64];
+            load_words<D / 64>(block + key_code, words);
+            load_words<D / 64>(block + key_scale_at<D>(r), scales);
+            load_words<D / 64>(block + value_code, value_codes);
+            load_words<D / 64>(block + value_scale_at<D>(r), value_scales);
+            from_key_words<D>(u, words, codes);
+            if (valid) {
+                dequantise<T, D>(codes, scales, u, k + src);
+                dequantise<T, D>(value_codes, value_scales, u, v + src);
+            }
         }
-        quantise<T, D>(nv, codes, scales);
-        if (valid) {
-            store_words<D / 64>(block + value_code_at<D>(r, u), codes);
-            if (u == 0) store_words<D / 64>(block + value_scale_at<D>(r), scales);
-        }
-    } else {
-        load_words<D / 64>(block + key_code_at<D>(r) + (u >> 1) * (D / 8) + (u & 1) * (D / 16), words);
-        load_words<D / 64>(block + key_scale_at<D>(r), scales);
-        from_key_words<D>(u, words, codes);
-        if (valid) dequantise<T, D>(codes, scales, u, k + src);
-        load_words<D / 64>(block + value_code_at<D>(r, u), codes);
-        load_words<D / 64>(block + value_scale_at<D>(r), scales);
-        if (valid) dequantise<T, D>(codes, scales, u, v + src);
     }
 }
 
 template <typename T, int D, bool WRITE>
 int launch_rows(const RowArgs& a, const void* k, const void* v, const void* kv4, cudaStream_t stream) {
     const int quads = (a.n_rows + kRowsPerWarp - 1) / kRowsPerWarp;
-    const long long items = (long long)quads * a.n_kv_heads * a.n_layers;
+    const long long warps = (long long)quads * a.n_kv_heads * a.n_layers;
+    // a warp finds its rows once for several heads, where that leaves every SM the warps it holds four times over (2.4 M rows of a
+    // head: writing with runs of 1, 2, 4, 8, 16 heads 415, 341, 302, 293, 301 us; reading 321, 286, 269, 274, 276)
+    const int run = (int)std::max(1LL, std::min({(long long)a.n_kv_heads, WRITE ? 8LL : 4LL, warps / (256LL * sm_count())}));
+    const int runs = (a.n_kv_heads + run - 1) / run;
+    const long long items = (long long)quads * runs * a.n_layers;
     if (items > 0x7fffffffLL - 64) return CF_ERR_INVALID_ARG;
     const unsigned blocks = (unsigned)((items + kRowThreads / 32 - 1) / (kRowThreads / 32));
-    return launch_chained(rows_kernel<T, D, WRITE>, dim3(blocks), kRowThreads, 0, stream, a, Divisor(a.page_rows), Divisor(a.n_kv_heads),
-                          Divisor(quads), static_cast<T*>(const_cast<void*>(k)), static_cast<T*>(const_cast<void*>(v)),
+    return launch_chained(rows_kernel<T, D, WRITE>, dim3(blocks), kRowThreads, 0, stream, a, Divisor(a.page_rows), Divisor(runs),
+                          Divisor(quads), run, static_cast<T*>(const_cast<void*>(k)), static_cast<T*>(const_cast<void*>(v)),
                           static_cast<unsigned char*>(const_cast<void*>(kv4)));
 }
 
