@@ -24,7 +24,7 @@
 #include <algorithm>
 #include <climits>
 
-#include "cf_kv4.cuh"
+#include "cf_kv4_attn.cuh"
 #include "cf_tc_util.cuh"
 
 namespace cf {
@@ -38,7 +38,8 @@ namespace {
 
 constexpr int kStages = 2;                        // steps of the ring
 constexpr int kStepBlocks = 2;                    // blocks of a step
-constexpr int kStepRows = kStepBlocks * kBlockRows;
+constexpr int kStepLog2 = 5, kStepRows = kStepBlocks * kBlockRows;
+static_assert(kStepRows == 1 << kStepLog2, "a step's keys");
 constexpr int kMergeThreads = 256;
 constexpr float kSlack = 8.f;                     // how far a logit may lie above the running maximum (base 2)
 constexpr int kHead = 7;                          // P is at most 2^kSlack * 2^kHead, below fp16's 2^16
@@ -48,6 +49,7 @@ constexpr int kMostCost = 32;                     // of a unit, in steps
 // the warps that have a share of their own, or the CTA that has one.
 constexpr int kLeastAlone = 4, kLeastTogether = 8;
 constexpr int kCostAlone = 3, kCostTogether = 16;
+constexpr int kLeastTc = 8, kCostTc = 6;          // of the tensor-core kernel, in steps of its own
 
 // Warps of a CTA, and CTAs of an SM.  With few columns the loop fits 128 registers: 16 warps per SM; without, and with twice the
 // columns, fewer warps with more registers are faster.
@@ -56,23 +58,6 @@ __host__ __device__ constexpr int ctas_per_sm(int nt, bool few) { return few ? 2
 
 // Query columns of a unit.
 __host__ __device__ constexpr int tile_columns(int head_dim, int nt, bool few) { return few ? 8 / (head_dim / 32) : 8 * nt; }
-
-struct Kv4Args {
-    const void* q;
-    const unsigned char* kv4;
-    void* out;
-    float* lse;
-    float* part_o;                                // [2 shares][columns][D]
-    float* part_ml;                               // [2 shares][2][columns]
-    int4* marks;                                  // for the merge, by unit or by share: parts, first share, layer * requests + request, unit
-    long long q_layer_stride, kv4_layer_stride, out_layer_stride;
-    int n_layers, q_len, n_q_heads, n_kv_heads, columns;                   // columns = query heads of a kv head * q_len
-    Divisor group, tiles, blocks_per_page;
-    int n_shares, warps_per_share, unit_cost;
-    int marks_by_unit;                            // a mark for every unit, where there are fewer units than shares
-    long long least_share;
-    float scale_log2;
-};
 
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
@@ -115,73 +100,6 @@ template <int N> __device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N
     if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(a));
     if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(a));
 }
-
-__device__ __forceinline__ int steps_of(int rows) { return max(1, (rows + kStepRows - 1) / kStepRows); }
-
-// A share's way along the line.  A unit is as long as its steps and what a unit costs besides, `cost` of them, which come first: so
-// that shares over many short units are not the last to end.
-struct Walk {
-    int layer, request, unit;                     // unit = kv head * tiles + tile, within (layer, request)
-    int rows, length;                             // rows of the request, length of the unit
-    int at;                                       // place in the unit
-    long long left;                               // of the share, from there on
-    __device__ __forceinline__ int end() const { return (int)min((long long)length, at + left); }
-    __device__ __forceinline__ int first_step(int cost) const { return max(0, at - cost); }
-    __device__ __forceinline__ int last_step(int cost) const { return max(0, end() - cost); }
-};
-
-struct Line {
-    const PagesView& pv;
-    int units, cost;                              // units per (layer, request)
-    int most;                                     // rows the table has room for
-    __device__ __forceinline__ int rows_of(int b) const { return min(max(pv.rows[b], 0), most); }
-    __device__ __forceinline__ long long length_of_layer() const {
-        long long sum = 0;
-#pragma unroll 4
-        for (int b = threadIdx.x & 31; b < pv.n_requests; b += 32) sum += steps_of(rows_of(b)) + cost;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        return sum * units;
-    }
-    __device__ __forceinline__ Walk find(long long at, long long left, long long per_layer) const {
-        const int lane = threadIdx.x & 31;
-        Walk p = {};
-        p.left = left;
-        if (at >= per_layer) p.layer = (int)(at / per_layer), at -= p.layer * per_layer;
-        for (int b0 = 0;; b0 += 32) {
-            const int b = b0 + lane, rows = b < pv.n_requests ? rows_of(b) : 0, length = b < pv.n_requests ? steps_of(rows) + cost : 0;
-            long long end = (long long)length * units;
-            const long long mine = end;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long x = __shfl_up_sync(0xffffffffu, end, o);
-                if (lane >= o) end += x;
-            }
-            const unsigned behind = __ballot_sync(0xffffffffu, end > at);
-            if (behind != 0 || b0 + 32 >= pv.n_requests) {
-                const int src = behind != 0 ? __ffs(behind) - 1 : 0;
-                p.request = b0 + src;
-                p.rows = __shfl_sync(0xffffffffu, rows, src);
-                p.length = __shfl_sync(0xffffffffu, length, src);
-                const int within = (int)(at - __shfl_sync(0xffffffffu, end - mine, src));    // the host has seen to 32 bits
-                p.unit = within / p.length;
-                p.at = within - p.unit * p.length;
-                return p;
-            }
-            at -= __shfl_sync(0xffffffffu, end, 31);
-        }
-    }
-    // To the beginning of the next unit; there is one where something is left.
-    __device__ __forceinline__ void next_unit(Walk& p) const {
-        p.left -= p.end() - p.at;
-        p.at = 0;
-        if (p.left <= 0 || ++p.unit < units) return;
-        p.unit = 0;
-        if (++p.request == pv.n_requests) p.request = 0, ++p.layer;
-        p.rows = rows_of(p.request);
-        p.length = steps_of(p.rows) + cost;
-    }
-};
 
 // The copies of a warp's steps: it takes every stride-th step from `first` on of each unit of its share.  The walk lies in shared
 // memory: it is looked at once in 32 steps.
@@ -261,30 +179,6 @@ struct Feeder {
 
 template <typename T> struct IsF32 { static constexpr bool value = sizeof(T) == 4; };
 
-template <typename T>
-__device__ __forceinline__ void store4(T* p, float a, float b, float c, float d);
-template <>
-__device__ __forceinline__ void store4<float>(float* p, float a, float b, float c, float d) {
-    *reinterpret_cast<float4*>(p) = make_float4(a, b, c, d);
-}
-template <>
-__device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16* p, float a, float b, float c, float d) {
-    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b), y = __floats2bfloat162_rn(c, d);
-    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-}
-
-// Results of a column: where they go, by the column's number within the kv head (token-major).
-template <typename T, int D>
-__device__ __forceinline__ T* out_row(const Kv4Args& a, int layer, int request, int head, int column) {
-    const int token = a.group.quotient(column), h = head * (int)a.group.d + a.group.remainder(column);
-    return static_cast<T*>(a.out) + (size_t)layer * a.out_layer_stride + (((size_t)request * a.q_len + token) * a.n_q_heads + h) * D;
-}
-__device__ __forceinline__ void store_lse(const Kv4Args& a, int n_requests, int layer, int request, int head, int column, float m, float l) {
-    if (!a.lse) return;
-    const int token = a.group.quotient(column), h = head * (int)a.group.d + a.group.remainder(column);
-    a.lse[(((size_t)layer * n_requests + request) * a.n_q_heads + h) * a.q_len + token] = l > 0.f || l != l ? m * kLn2 + logf(l) : -INFINITY;
-}
-
 // FEW: the query columns times the groups fit the eight columns of a matrix product, which then has a column per (query, group):
 // one chain of products for all groups, and one set of probabilities instead of one per group.
 template <typename T, int D, int NT, bool FEW>
@@ -321,7 +215,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
     const bool together = a.warps_per_share > 1;             // the CTA's warps share a share
     const int share = together ? (int)blockIdx.x : (int)blockIdx.x * kWarps + warp;
     const int cost = a.unit_cost;
-    const Line line = {pv, a.n_kv_heads * (int)a.tiles.d, cost, pv.table_cols * pv.page_rows};
+    const Line line = {pv, a.n_kv_heads * (int)a.tiles.d, cost, pv.table_cols * pv.page_rows, kStepLog2};
     const long long per_layer = line.length_of_layer(), total = per_layer * a.n_layers;
     const long long size = max(a.least_share, (total + a.n_shares - 1) / a.n_shares);
     const long long begin = share * size, mine = min(size, total - begin);
@@ -804,6 +698,7 @@ kv4_merge_kernel(Kv4Args args, PagesView pv, Divisor requests, int tile, int col
 
 // How a call is cut: everything the host can know of it.
 struct Cut {
+    bool tc;                                      // the tensor-core kernel
     int nt;                                       // products of eight columns that a warp takes
     bool few;
     int tile, tiles, columns;                     // columns of a unit, units and columns of a kv head
@@ -818,6 +713,8 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
     c.nt = c.columns <= 8 ? 1 : 2;
     c.few = c.columns <= tile_columns(g->head_dim, 1, true);
     c.tile = tile_columns(g->head_dim, c.nt, c.few);
+    c.tc = kv4_attn_tc_supported(g, c.columns);
+    if (c.tc) c.tile = kTcColumns;
     c.tiles = (c.columns + c.tile - 1) / c.tile;
     c.warps = warps_of(c.few);
     c.ctas = sm_count() * ctas_per_sm(c.nt, c.few);
@@ -828,6 +725,10 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
     const double units = (double)n_layers * p->n_requests * g->n_kv_heads * c.tiles;
     c.warps_per_share = 5.0 * units >= (double)c.ctas * c.warps ? 1 : c.warps;
     c.n_shares = c.warps_per_share == 1 ? c.ctas * c.warps : c.ctas;
+    if (c.tc) {                                   // a CTA per SM and share
+        c.ctas = c.n_shares = sm_count();
+        c.warps_per_share = c.warps;
+    }
     c.marks_by_unit = units <= c.n_shares;
     c.marks = c.marks_by_unit ? (int)units : c.n_shares;
     return c;
@@ -853,16 +754,9 @@ size_t attn_smem(int head_dim, int warps, int tile) {
            (size_t)warps * kStages * 8;
 }
 
-template <typename T, int D, int NT, bool FEW>
-int launch_attn(const Kv4Args& a, const PagesView& pv, int ctas, int marks, cudaStream_t stream) {
-    static PerDeviceOnce once;
-    const size_t smem = attn_smem(D, warps_of(FEW), tile_columns(D, NT, FEW));
-    const int rc = configure_smem_once(once, kv4_attn_kernel<T, D, NT, FEW>, (int)smem);
-    if (rc != CF_OK) return rc;
-    const int err = launch_chained(kv4_attn_kernel<T, D, NT, FEW>, dim3((unsigned)ctas), 32 * warps_of(FEW), smem, stream, a, pv);
-    if (err != CF_OK) return err;
+template <typename T, int D>
+int launch_merge(const Kv4Args& a, const PagesView& pv, int tile, int marks, cudaStream_t stream) {
     // a block takes all columns of a unit where units are many, fewer where they are not
-    constexpr int tile = tile_columns(D, NT, FEW);
     int cols = std::min(tile, kMergeThreads / (D / 4));
     while (cols > 1 && marks * (tile / cols) < 2 * sm_count()) cols /= 2;
     int lanes_log2 = 0;
@@ -871,10 +765,20 @@ int launch_attn(const Kv4Args& a, const PagesView& pv, int ctas, int marks, cuda
                           Divisor(pv.n_requests), tile, cols, lanes_log2);
 }
 
+template <typename T, int D, int NT, bool FEW>
+int launch_attn(const Kv4Args& a, const PagesView& pv, const Cut& c, cudaStream_t stream) {
+    static PerDeviceOnce once;
+    const size_t smem = attn_smem(D, warps_of(FEW), tile_columns(D, NT, FEW));
+    const int rc = configure_smem_once(once, kv4_attn_kernel<T, D, NT, FEW>, (int)smem);
+    if (rc != CF_OK) return rc;
+    const int err = launch_chained(kv4_attn_kernel<T, D, NT, FEW>, dim3((unsigned)c.ctas), 32 * warps_of(FEW), smem, stream, a, pv);
+    return err != CF_OK ? err : launch_merge<T, D>(a, pv, c.tile, c.marks, stream);
+}
+
 template <typename T, int D>
 int launch_attn_cut(const Kv4Args& a, const PagesView& pv, const Cut& c, cudaStream_t stream) {
-    if (c.few) return launch_attn<T, D, 1, true>(a, pv, c.ctas, c.marks, stream);
-    return c.nt == 1 ? launch_attn<T, D, 1, false>(a, pv, c.ctas, c.marks, stream) : launch_attn<T, D, 2, false>(a, pv, c.ctas, c.marks, stream);
+    if (c.few) return launch_attn<T, D, 1, true>(a, pv, c, stream);
+    return c.nt == 1 ? launch_attn<T, D, 1, false>(a, pv, c, stream) : launch_attn<T, D, 2, false>(a, pv, c, stream);
 }
 
 template <typename T>
@@ -929,9 +833,14 @@ int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, in
     a.n_shares = c.n_shares, a.warps_per_share = c.warps_per_share, a.marks_by_unit = c.marks_by_unit;
     a.least_share = c.warps_per_share == 1 ? kLeastAlone : kLeastTogether;
     a.unit_cost = c.warps_per_share == 1 ? kCostAlone : kCostTogether;
+    if (c.tc) a.least_share = kLeastTc, a.unit_cost = kCostTc;
     a.scale_log2 = scale * kLog2e;
     const PagesView pv = make_pages_view(pages);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (c.tc) {
+        const int err = launch_kv4_attn_tc(a, pv, s);
+        return err != CF_OK ? err : launch_merge<__nv_bfloat16, 128>(a, pv, c.tile, c.marks, s);
+    }
     return geom->dtype == CF_BF16 ? launch_attn_typed<__nv_bfloat16>(a, pv, c, geom->head_dim, s)
                                   : launch_attn_typed<float>(a, pv, c, geom->head_dim, s);
 }

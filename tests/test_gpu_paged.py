@@ -425,3 +425,72 @@ def test_a_decoding_loop_over_the_caches_that_pruning_left(marshal, monkeypatch)
                 whole = [torch.cat([c[l, b, :n], x[:t + 1, l, b, 0]]).double().cpu().numpy() for c, x in ((k_fin, k_new), (v_fin, v_new))]
                 kept[-1].append([P.numbers(*P.quantise(x)) for x in whole])
         _check_attention(sess.geom, out[t], lse[t], q_new[t], kept, d ** -0.5)
+
+
+@pytest.mark.parametrize("hq,hkv,lengths,page_rows,q_len,layers", [
+    (12, 2, [64], 64, 16, 1), (28, 4, [130, 24, 10, 0], 32, 24, 1), (4, 4, [500, 33], 48, 40, 2), (64, 4, [300, 5], 16, 9, 1),
+    (8, 1, [1500], 80, 33, 1), (7, 1, [63, 64, 65, 127, 128, 129], 16, 19, 1), (28, 4, [40 * i % 333 for i in range(40)], 16, 5, 1),
+    (16, 2, [9000, 3], 64, 100, 1)],
+    ids=lambda x: str(x) if isinstance(x, int) else "%dx%d" % (len(x), max(x)))
+def test_attention_of_many_query_columns(hq, hkv, lengths, page_rows, q_len, layers):
+    """The tensor-core kernel: one and several tiles of columns, the last one with columns that are none, ends of requests inside and
+    between tiles and pages, queries that see nothing."""
+    geom = cf.make_geom(hq, hkv, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, hkv, 128, lengths, page_rows, layers, seed=q_len)
+    q = torch.randn((layers, len(lengths), q_len, hq, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    torch.cuda.synchronize()
+    assert cf.cf_pages_status(pages.desc) == 0
+    _check_attention(geom, out, lse, q, kept, 128 ** -0.5)
+    again, lse2 = _attend(geom, pages, pool, q)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("q_scale,softmax_scale", [(1e-20, 1e19), (3e4, 3e-5), (60.0, 0.0), (1e30, 1e-31), (0.0, 0.0), (5.0, -0.2)])
+def test_many_queries_of_any_size(q_scale, softmax_scale):
+    geom = cf.make_geom(6, 2, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, 2, 128, [333, 50], 32, 1, seed=9)
+    q = (torch.randn((1, 2, 20, 6, 128), generator=torch.Generator().manual_seed(4)) * q_scale).to(torch.bfloat16).cuda()
+    out, lse = _attend(geom, pages, pool, q, softmax_scale)
+    _check_attention(geom, out, lse, q, kept, softmax_scale or 128 ** -0.5)
+
+
+def test_many_queries_over_keys_and_values_of_any_size():
+    """Scales that grow and shrink along a request, tile by tile and inside tiles."""
+    geom = cf.make_geom(4, 1, 128, torch.bfloat16, 32768, 1e6)
+    lengths = [300, 300, 300]
+    pages, pool, _ = _filled(geom, 1, 128, lengths, 16, 1, seed=2)
+    rows = torch.arange(300, device="cuda")
+    slots = torch.stack([pages.table[b, rows // 16].long() * 16 + rows % 16 for b in range(3)])
+    gen = torch.Generator().manual_seed(1)
+    k, v = torch.randn((1, 3, 300, 1, 128), generator=gen), torch.randn((1, 3, 300, 1, 128), generator=gen)
+    v[0, 0] *= 2.0 ** torch.linspace(-30, 10, 300)[:, None, None]
+    v[0, 1] *= 2.0 ** torch.linspace(10, -30, 300)[:, None, None]
+    v[0, 2] *= 1e-30
+    k[0, 1] *= 2.0 ** torch.linspace(-12, 2, 300)[:, None, None]
+    k[0, 2, 100:116] *= 2.0 ** torch.linspace(-10, 3, 16)[:, None, None]
+    k, v = k.bfloat16(), v.bfloat16()
+    cf.cf_kv4_write(geom, pages.desc, pool, slots, k.cuda(), v.cuda())
+    kept = [[[P.numbers(*P.quantise(x[0, b].double().numpy())) for x in (k, v)] for b in range(3)]]
+    q = torch.randn((1, 3, 12, 4, 128), generator=gen).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    _check_attention(geom, out, lse, q, kept, 128 ** -0.5)
+
+
+def test_many_queries_and_numbers_that_are_not_finite():
+    geom = cf.make_geom(2, 1, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, 1, 128, [140, 40], 16, 1, seed=5)
+    k, v = torch.randn((1, 1, 1, 128)).bfloat16(), torch.randn((1, 1, 1, 128)).bfloat16()
+    v[..., 70] = float("inf")
+    slot = int(pages.table[0, 130 // 16]) * 16 + 130 % 16
+    cf.cf_kv4_write(geom, pages.desc, pool, torch.tensor([slot], device="cuda"), k.cuda(), v.cuda())
+    q = torch.randn((1, 2, 20, 2, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    want = torch.zeros((2, 20, 2, 128), dtype=torch.bool)
+    want[0, 10:, :, 64:96] = True                   # row 130 of 140 is seen by the last ten of twenty queries
+    assert torch.equal(torch.isnan(out[0]).cpu(), want) and torch.isfinite(lse).all()
+    k[..., 3] = float("nan")
+    cf.cf_kv4_write(geom, pages.desc, pool, torch.tensor([slot], device="cuda"), k.cuda(), torch.zeros_like(v).cuda())
+    out, lse = _attend(geom, pages, pool, q)
+    want[0, 10:] = True
+    assert torch.equal(torch.isnan(out[0]).cpu(), want) and torch.equal(torch.isnan(lse[0, 0]).cpu(), want[0, :, :, 0].T)
