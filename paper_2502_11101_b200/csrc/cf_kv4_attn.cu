@@ -713,7 +713,8 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
     c.nt = c.columns <= 8 ? 1 : 2;
     c.few = c.columns <= tile_columns(g->head_dim, 1, true);
     c.tile = tile_columns(g->head_dim, c.nt, c.few);
-    c.tc = kv4_attn_tc_supported(g, c.columns);
+    const double heads = (double)n_layers * p->n_requests * g->n_kv_heads;
+    c.tc = kv4_attn_tc_supported(g, c.columns, heads * ((c.columns + kTcColumns - 1) / kTcColumns));
     if (c.tc) c.tile = kTcColumns;
     c.tiles = (c.columns + c.tile - 1) / c.tile;
     c.warps = warps_of(c.few);
@@ -722,10 +723,10 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
     // of their own with 3 steps for every unit and every share.  With U units and W warps: 16 U against 3 (U + W).
     // Measured (together / alone, us): 96 requests, 28/4 (U = 0.22 W) 46.7 / 44.9; 512 short ones, 32/8 (2.3 W) 94.6 / 39.4;
     // 3 requests, four layers, 32/8 (0.05 W) 17.3 / 21.2; 8 long ones, 32/32 (0.11 W) 122 / 126.
-    const double units = (double)n_layers * p->n_requests * g->n_kv_heads * c.tiles;
+    const double units = heads * c.tiles;
     c.warps_per_share = 5.0 * units >= (double)c.ctas * c.warps ? 1 : c.warps;
     c.n_shares = c.warps_per_share == 1 ? c.ctas * c.warps : c.ctas;
-    if (c.tc) {                                   // a CTA per SM and share
+    if (c.tc) {                                   // a share to a CTA, one to an SM
         c.ctas = c.n_shares = sm_count();
         c.warps_per_share = c.warps;
     }

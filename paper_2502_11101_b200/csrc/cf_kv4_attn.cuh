@@ -121,7 +121,7 @@ __device__ __forceinline__ void store_lse(const Kv4Args& a, int n_requests, int 
 
 // The tensor-core kernel (cf_kv4_attn_tc.cu): units of kTcColumns query columns, steps of 1 << kTcStepLog2 keys, a CTA per share.
 constexpr int kTcColumns = 128, kTcStepLog2 = 6;
-bool kv4_attn_tc_supported(const cf_geom* g, int columns);
+bool kv4_attn_tc_supported(const cf_geom* g, int columns, double units);
 int launch_kv4_attn_tc(const kv4::Kv4Args& a, const PagesView& pv, cudaStream_t stream);
 
 }  // namespace cf

@@ -3,13 +3,17 @@
 // verification of drafted tokens.
 //
 // A unit is 128 query columns of a (layer, request, kv head) and the request's rows, 64 at a time.  Roles of a CTA:
-//   warps 0-3   softmax, one query column per thread (= TMEM lane); its queries into tensor memory, its results out of it
-//   warps 4-7   codes to fp16 keys, 16 rows each, into a swizzled shared-memory tile
-//   warps 8-11  codes to fp16 values
-//   warp 12     MMA issue, the warp converged and one lane elected
-//   warp 13     copies of the pool's blocks
-// S = Q K^T with the queries as the A operand in tensor memory, O += P V with P as the A operand over the S columns already
-// consumed; two S buffers, so that S of the next tile is computed while the softmax is at this one.
+//   warps 0-7   softmax, one query column per thread (= TMEM lane), two groups of four warps on tiles in turn; the queries into
+//               tensor memory, the results out of it, half of the dims each
+//   warps 8-11  codes to fp16 keys, 16 rows each, into a swizzled shared-memory tile
+//   warps 12-15 codes to fp16 values
+//   warp 16     MMA issue, the warp converged and one lane elected
+//   warp 17     copies of the pool's blocks
+// S = Q K^T with the queries as the A operand in tensor memory, O += P V with P as the A operand, there too; four S buffers and two
+// of P, so that QK^T runs two tiles ahead and neither group waits for it.  A group reads its tile's S twice, for the maximum and for the probabilities; what
+// probabilities are taken from (`base`) goes from tile to tile, so a group has to wait for the other's maximum, not for its
+// probabilities.  (One group with two S buffers 52 us, two threads to a column 51, two CTAs of one group per SM 58; this one: see
+// launch_kv4_attn_tc.)
 // Numbers: a code times its scale is ten bits, exact in fp16 as long as the scales of a block of 16 rows lie within 2^28 of each
 // other: a block is kept in units of 2^c, c chosen so that its largest scale comes to lie in [2^12, 2^13) (smaller ones lose last
 // bits, 2^-38 of the block's largest number and less).  Keys' units go into the logits' factor, which is the same for the 16
@@ -34,22 +38,46 @@ constexpr int kRaw = 3;                           // tiles of raw blocks
 constexpr int kKeys = 1 << kTcStepLog2, kBlocks = kKeys / kBlockRows;
 constexpr int kKeyHalf = kKeys * 128, kKeyTile = 2 * kKeyHalf;     // bytes: 64 dims of a tile, a tile
 constexpr int kBlockBytes = block_bytes(kD), kRawTile = kBlocks * kBlockBytes;
-constexpr int kMmaWarp = 12, kLoadWarp = 13, kTcThreads = 448;
-constexpr int kUnits = 4;                         // rings of the blocks' units (keys run three tiles ahead of the softmax) and of NaN marks
+constexpr int kTiles = 4;                         // of keys and of values
+constexpr int kAhead = 2;                         // tiles that QK^T runs ahead of PV
+constexpr int kKeyWarp = 8, kValueWarp = 12, kMmaWarp = 16, kLoadWarp = 17, kTcThreads = 576;
+constexpr int kUnits = 8;                         // rings of what goes with a tile (keys run four tiles ahead of the softmax), and of NaN marks
 constexpr float kSlack = 8.f;
 constexpr int kHead = 7;                          // P is at most 2^kSlack * 2^kHead, below fp16's 2^16
-constexpr int kTmemS = 0, kTmemO = 128, kTmemQ = 256, kTmemColumns = 512;
+constexpr int kTmemS = 0, kTmemO = 256, kTmemQ = 384, kTmemP = 448, kTmemColumns = 512;   // four S buffers, two of P
 
 struct TcShared {
-    unsigned long long raw_full[kRaw], raw_free[kRaw], k_full[2], v_full[2], s_full[2], p_ready[2], o_done[2], q_full;
+    unsigned long long raw_full[kRaw], raw_free[kRaw], full[kTiles], k_free[kTiles], v_free[kTiles], s_full[4], p_ready[2], o_done[2], q_full;
+    unsigned long long based[4], exchanged[4];    // by 32 query columns: the base of a tile is known; what the groups tell each other at the end
     unsigned tmem_base;
     volatile int abort_flag;
     float key_unit[kUnits][kBlocks];              // 2^c of a tile's blocks
     int value_unit[kUnits][kBlocks];              // c
+    int o_unit[2];                                // of O, by the last tiles of the two groups
+    float base[2][kTcColumns];                    // of the last tiles of the two groups; -infinity: no key seen yet
+    float row[2][2][kTcColumns];                  // by parity of the exchange and group
     volatile int nan_unit[kUnits];                // by ordinal: that + 1 where a unit has a NaN among the values that not all of its queries see
 };
-constexpr int kTcSmem = 1024 + 4 * kKeyTile + kRaw * kRawTile + (int)sizeof(TcShared);
+constexpr int kTcSmem = 1024 + 2 * kTiles * kKeyTile + kRaw * kRawTile + (int)sizeof(TcShared);
 
+// A bounded wait of a whole warp, the same answer in every lane: three instructions a turn, of which there are a hundred for each
+// tile among eighteen warps (with a look at the clock and the abort flag in every turn waiting took two fifths of the issue
+// slots).  The limit is a number of turns, each of which the hardware holds for a hundred cycles or so.
+constexpr uint32_t kWaitTurns = 1u << 23;
+__device__ __forceinline__ bool role_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p, more;\n.reg .u32 n;\nmov.u32 n, 0;\n"
+        "AGAIN:\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n@p bra.uni DONE;\n"
+        "add.u32 n, n, 1;\nsetp.lt.u32 more, n, %3;\n@more bra.uni AGAIN;\n"
+        "DONE:\nselp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "n"(kWaitTurns)
+        : "memory");
+    if (__all_sync(0xffffffffu, ok != 0)) return true;
+    *abort_flag = 1;
+    return false;
+}
 // fp16 x fp16 -> fp32, A and K-major B; B may be MN-major.
 __device__ __forceinline__ uint32_t instr_desc_f16(int n, bool b_mn_major) {
     return (1u << 4) | (b_mn_major ? (1u << 16) : 0u) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kTcColumns >> 4) << 24);
@@ -127,8 +155,8 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
     chain_next();
     chain_wait();
     const Kv4Args& a = args;
-    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    unsigned char *s_k = smem, *s_v = smem + 2 * kKeyTile, *s_raw = smem + 4 * kKeyTile;
+    unsigned char* smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
+    unsigned char *s_k = smem, *s_v = smem + kTiles * kKeyTile, *s_raw = smem + 2 * kTiles * kKeyTile;
     TcShared* sh = reinterpret_cast<TcShared*>(s_raw + kRaw * kRawTile);
     volatile int* abort_flag = &sh->abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -151,14 +179,21 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 mbar_init(smem_u32(&sh->raw_full[i]), kBlocks);
                 mbar_init(smem_u32(&sh->raw_free[i]), 2 * kBlocks);
             }
+            for (int i = 0; i < kTiles; ++i) {
+                mbar_init(smem_u32(&sh->full[i]), 2 * kBlocks);
+                mbar_init(smem_u32(&sh->k_free[i]), 1);
+                mbar_init(smem_u32(&sh->v_free[i]), 1);
+            }
+            for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&sh->s_full[i]), 1);
             for (int i = 0; i < 2; ++i) {
-                mbar_init(smem_u32(&sh->k_full[i]), kBlocks);
-                mbar_init(smem_u32(&sh->v_full[i]), kBlocks);
-                mbar_init(smem_u32(&sh->s_full[i]), 1);
                 mbar_init(smem_u32(&sh->p_ready[i]), 4);
                 mbar_init(smem_u32(&sh->o_done[i]), 1);
             }
-            mbar_init(smem_u32(&sh->q_full), 4);
+            for (int i = 0; i < 4; ++i) {
+                mbar_init(smem_u32(&sh->based[i]), 1);
+                mbar_init(smem_u32(&sh->exchanged[i]), 2);
+            }
+            mbar_init(smem_u32(&sh->q_full), 8);
             sh->abort_flag = 0;
             for (int i = 0; i < kUnits; ++i) sh->nan_unit[i] = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -197,7 +232,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 }
                 for (int i = 0; ok && i < min(8, last - t0); ++i, ++g) {
                     const int stage = g % kRaw;
-                    if (g >= kRaw) ok = warp_wait(smem_u32(&sh->raw_free[stage]), (g / kRaw - 1) & 1, abort_flag);
+                    if (g >= kRaw) ok = role_wait(smem_u32(&sh->raw_free[stage]), (g / kRaw - 1) & 1, abort_flag);
                     if (ok && (lane >> 2) == i) {
                         const uint32_t bar = smem_u32(&sh->raw_full[stage]);
                         if (from) {
@@ -216,43 +251,48 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
         const uint64_t dk = smem_desc(smem_u32(s_k), 16, 1024), dv = smem_desc(smem_u32(s_v), kKeyHalf, 1024);
         const uint32_t idesc_s = instr_desc_f16(kKeys, false), idesc_o = instr_desc_f16(kD, true);
         auto issue_pv = [&](int tile, bool first) {          // O (+)= P V of a tile
-            const int b = tile & 1;
-            ok = warp_wait(smem_u32(&sh->v_full[b]), (tile >> 1) & 1, abort_flag) && warp_wait(smem_u32(&sh->p_ready[b]), (tile >> 1) & 1, abort_flag);
+            const int b = tile & 1, v = tile % kTiles;
+            ok = role_wait(smem_u32(&sh->p_ready[b]), (tile >> 1) & 1, abort_flag);
             if (!ok) return;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
                 for (int kk = 0; kk < kBlocks; ++kk)         // 16 keys = 8 packed P columns per instruction
-                    umma_ts(tmem + kTmemO, tmem + kTmemS + b * kKeys + kk * 8, dv + (uint64_t)(b * (kKeyTile >> 4) + kk * 128), idesc_o, first && kk == 0 ? 0u : 1u);
+                    umma_ts(tmem + kTmemO, tmem + kTmemP + b * (kKeys / 2) + kk * 8, dv + (uint64_t)(v * (kKeyTile >> 4) + kk * 128), idesc_o, first && kk == 0 ? 0u : 1u);
                 umma_commit(smem_u32(&sh->o_done[b]));
+                umma_commit(smem_u32(&sh->v_free[v]));
             }
             __syncwarp();
         };
         for (; ok && p.left > 0; line.next_unit(p)) {
             const int start = p.first_step(cost), last = p.last_step(cost);
             if (last <= start) continue;
-            ok = warp_wait(smem_u32(&sh->q_full), ordinal & 1, abort_flag);
-            for (int t = start; ok && t < last; ++t, ++g) {
-                const int b = g & 1;
-                ok = warp_wait(smem_u32(&sh->k_full[b]), (g >> 1) & 1, abort_flag);
-                if (!ok) break;
-                tc_fence_after();
-                if (elect_one()) {
+            ok = role_wait(smem_u32(&sh->q_full), ordinal & 1, abort_flag);
+            for (int t = start; ok && t < last + kAhead; ++t) {
+                if (t < last) {
+                    const int k = g % kTiles;
+                    // the values too: with S the softmax has the units of both
+                    ok = role_wait(smem_u32(&sh->full[k]), (g / kTiles) & 1, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {                       // over S of the tile four before, whose P has been waited for
 #pragma unroll
-                    for (int kk = 0; kk < 8; ++kk)
-                        umma_ts(tmem + kTmemS + b * kKeys, tmem + kTmemQ + kk * 8,
-                                dk + (uint64_t)((b * kKeyTile + (kk >> 2) * kKeyHalf + (kk & 3) * 32) >> 4), idesc_s, kk > 0);
-                    umma_commit(smem_u32(&sh->s_full[b]));
+                        for (int kk = 0; kk < 8; ++kk)
+                            umma_ts(tmem + kTmemS + (g & 3) * kKeys, tmem + kTmemQ + kk * 8,
+                                    dk + (uint64_t)((k * kKeyTile + (kk >> 2) * kKeyHalf + (kk & 3) * 32) >> 4), idesc_s, kk > 0);
+                        umma_commit(smem_u32(&sh->s_full[g & 3]));
+                        umma_commit(smem_u32(&sh->k_free[k]));
+                    }
+                    __syncwarp();
+                    ++g;
                 }
-                __syncwarp();
-                if (t > start) issue_pv(g - 1, t - 1 == start);
+                if (t - kAhead >= start) issue_pv(g - (min(t + 1, last) - (t - kAhead)), t - kAhead == start);
             }
-            if (ok) issue_pv(g - 1, last - 1 == start);
             ++ordinal;
         }
-    } else if (warp >= 4) {
+    } else if (warp >= kKeyWarp) {
         // -------------------------------------------------------------- codes to numbers
-        const bool values = warp >= 8;
+        const bool values = warp >= kValueWarp;
         const int block = warp & 3;
         for (; ok && p.left > 0; line.next_unit(p)) {
             const int start = p.first_step(cost), last = p.last_step(cost);
@@ -260,37 +300,51 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
             const int head = a.tiles.quotient(p.unit);
             const int all_see = p.rows - a.q_len + 1 + a.group.quotient((p.unit - head * (int)a.tiles.d) * kTcColumns);
             for (int t = start; ok && t < last; ++t, ++g) {
-                const int b = g & 1, stage = g % kRaw, row0 = t * kKeys + block * kBlockRows;
-                ok = warp_wait(smem_u32(&sh->raw_full[stage]), (g / kRaw) & 1, abort_flag);
-                // the tile before the last in this buffer has been read
-                if (ok && g >= 2) ok = warp_wait(smem_u32(values ? &sh->o_done[b] : &sh->s_full[b]), ((g >> 1) - 1) & 1, abort_flag);
+                const int k = g % kTiles, stage = g % kRaw, row0 = t * kKeys + block * kBlockRows;
+                ok = role_wait(smem_u32(&sh->raw_full[stage]), (g / kRaw) & 1, abort_flag);
+                // the tile that was in this buffer has been read
+                if (ok && g >= kTiles) ok = role_wait(smem_u32(values ? &sh->v_free[k] : &sh->k_free[k]), (g / kTiles - 1) & 1, abort_flag);
                 if (!ok) break;
                 const unsigned char* raw = s_raw + stage * kRawTile + block * kBlockBytes;
                 bool nan;
                 if (values) {
-                    const int unit = expand_block<true>(raw, s_v + b * kKeyTile, block, p.rows - row0, all_see - row0, nan);
+                    const int unit = expand_block<true>(raw, s_v + k * kKeyTile, block, p.rows - row0, all_see - row0, nan);
                     if (lane == 0) sh->value_unit[g % kUnits][block] = unit;
                     if (nan && lane == 0) sh->nan_unit[ordinal % kUnits] = ordinal + 1;
                 } else {
-                    const int unit = expand_block<false>(raw, s_k + b * kKeyTile, block, p.rows - row0, 0, nan);
+                    const int unit = expand_block<false>(raw, s_k + k * kKeyTile, block, p.rows - row0, 0, nan);
                     if (lane == 0) sh->key_unit[g % kUnits][block] = __int_as_float((127 + unit) << 23);
                 }
                 fence_proxy_async();
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(smem_u32(&sh->raw_free[stage]));
-                    mbar_arrive(smem_u32(values ? &sh->v_full[b] : &sh->k_full[b]));
+                    mbar_arrive(smem_u32(&sh->full[k]));
                 }
             }
             ++ordinal;
         }
     } else {
-        // -------------------------------------------------------------- softmax, one query column per thread
-        const uint32_t lane_tmem = tmem + ((uint32_t)(warp * 32) << 16);
+        // -------------------------------------------------------------- softmax, one query column per thread, tiles in turn
+        const int group = warp >> 2, quad = warp & 3, r = tid & (kTcColumns - 1);
+        const uint32_t lane_tmem = tmem + ((uint32_t)(quad * 32) << 16), p_addr = lane_tmem + kTmemP + group * (kKeys / 2);
+        // logits rise with q . k: the sign of the scale goes into the queries
+        const float scale = fabsf(a.scale_log2);
+        const uint32_t sign = a.scale_log2 < 0.f ? 0x80008000u : 0u;
+        int exchanges = 0;
+        // What the other group's thread of the column gives for `mine`.
+        auto exchange = [&](float mine) {
+            const int turn = exchanges++ & 1;
+            sh->row[turn][group][r] = mine;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->exchanged[quad]));
+            ok = role_wait(smem_u32(&sh->exchanged[quad]), turn, abort_flag);
+            return sh->row[turn][group ^ 1][r];
+        };
         for (; ok && p.left > 0; line.next_unit(p)) {
             const int start = p.first_step(cost), last = p.last_step(cost);
             if (last <= start) continue;
-            const int head = a.tiles.quotient(p.unit), col0 = (p.unit - head * (int)a.tiles.d) * kTcColumns, column = col0 + tid;
+            const int head = a.tiles.quotient(p.unit), col0 = (p.unit - head * (int)a.tiles.d) * kTcColumns, column = col0 + r;
             const bool real = column < a.columns;
             const int token = a.group.quotient(min(column, a.columns - 1));
             const int all_see = p.rows - a.q_len + 1 + a.group.quotient(col0), sees = p.rows - a.q_len + 1 + token;
@@ -299,140 +353,194 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
             {
                 const __nv_bfloat16* q = static_cast<const __nv_bfloat16*>(a.q) + (size_t)p.layer * a.q_layer_stride +
                                          (((size_t)p.request * a.q_len + token) * a.n_q_heads + head * (int)a.group.d + a.group.remainder(min(column, a.columns - 1))) * kD;
-                uint4 w[16];
+                uint4 w[8];
                 uint32_t amax = 0;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    w[i] = real ? *reinterpret_cast<const uint4*>(q + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
-                    const uint32_t m = __vmaxu2(__vmaxu2(w[i].x & 0x7fff7fffu, w[i].y & 0x7fff7fffu), __vmaxu2(w[i].z & 0x7fff7fffu, w[i].w & 0x7fff7fffu));
-                    amax = max(amax, max(m & 0xffffu, m >> 16));
-                }
+                for (int h = 0; h < 2; ++h)                  // both halves of the dims for the maximum, this group's last, to keep
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        w[i] = real ? *reinterpret_cast<const uint4*>(q + (h == 0 ? group ^ 1 : group) * (kD / 2) + 8 * i) : make_uint4(0u, 0u, 0u, 0u);
+                        const uint32_t m = __vmaxu2(__vmaxu2(w[i].x & 0x7fff7fffu, w[i].y & 0x7fff7fffu), __vmaxu2(w[i].z & 0x7fff7fffu, w[i].w & 0x7fff7fffu));
+                        amax = max(amax, max(m & 0xffffu, m >> 16));
+                    }
                 int e = amax == 0 || amax >= 0x7f80u ? 0 : (int)(amax >> 7) - 127;
                 e = max(-126, min(126, e));
                 const float down = __int_as_float((127 - e) << 23);
-                cs = a.scale_log2 * __int_as_float((127 + e) << 23);
+                cs = scale * __int_as_float((127 + e) << 23);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < 2; ++i) {
                     uint32_t f[16];
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const uint4 u = w[4 * i + x];
-                        f[4 * x] = pack_f16(bf16_low(u.x) * down, bf16_high(u.x) * down), f[4 * x + 1] = pack_f16(bf16_low(u.y) * down, bf16_high(u.y) * down);
-                        f[4 * x + 2] = pack_f16(bf16_low(u.z) * down, bf16_high(u.z) * down), f[4 * x + 3] = pack_f16(bf16_low(u.w) * down, bf16_high(u.w) * down);
+                        const uint32_t u[4] = {w[4 * i + x].x, w[4 * i + x].y, w[4 * i + x].z, w[4 * i + x].w};
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) f[4 * x + y] = pack_f16(bf16_low(u[y]) * down, bf16_high(u[y]) * down) ^ sign;
                     }
-                    tmem_st16_from<0>(lane_tmem + kTmemQ + 16 * i, f);
+                    tmem_st16_from<0>(lane_tmem + kTmemQ + group * (kD / 4) + 16 * i, f);
                 }
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&sh->q_full));
             }
-            float base = 0.f, slack = -INFINITY, l = 0.f;    // as in the other kernel: the running maximum (0 before there is one), room above it
-            int o_unit = 0;
-            for (int t = start; ok && t < last; ++t, ++g) {
-                const int b = g & 1;
-                const uint32_t s_addr = lane_tmem + kTmemS + b * kKeys;
-                // (not for k_full: the keys of tile g + 2 may be there before this warp looks, and a parity wait would miss the phase.  S of
-                // g + 2 waits for this tile's P, and so do the values of g + 2.)
-                ok = warp_wait(smem_u32(&sh->v_full[b]), (g >> 1) & 1, abort_flag) && warp_wait(smem_u32(&sh->s_full[b]), (g >> 1) & 1, abort_flag);
+            // what the probabilities of the group's last tile were taken from (-infinity: no key seen), and their sum
+            float base = -INFINITY, l = 0.f;
+            int o_unit = -1000;                              // of the tile before, in either group
+            for (int t = start; t < last; ++t, ++g) {
+                if ((g & 1) != group) continue;
+                const int* value_unit = sh->value_unit[g % kUnits];
+                const float* key_unit = sh->key_unit[g % kUnits];
+                const uint32_t s_addr = lane_tmem + kTmemS + (g & 3) * kKeys;
+                ok = role_wait(smem_u32(&sh->s_full[g & 3]), (g >> 2) & 1, abort_flag);
                 if (!ok) break;
                 tc_fence_after();
-                float x[kBlocks][16];
-#pragma unroll
-                for (int c = 0; c < kBlocks; ++c) tmem_ld16_async(s_addr + 16 * c, reinterpret_cast<uint32_t(&)[16]>(x[c]));
-                float most = -INFINITY;
-                int unit[kBlocks], top_unit = -1000;
                 const bool masked = (t + 1) * kKeys > all_see;
+                // the largest logit: S is read once for it and once for the probabilities
+                float most = -INFINITY;
+                int top_unit = -1000;
 #pragma unroll
-                for (int c = 0; c < kBlocks; ++c) {
-                    const float f = cs * sh->key_unit[g % kUnits][c];
-                    unit[c] = sh->value_unit[g % kUnits][c];
-                    top_unit = max(top_unit, unit[c]);
-                    tmem_ld16_wait(reinterpret_cast<uint32_t(&)[16]>(x[c]));
-                    if (!masked) {
+                for (int c = 0; c < kBlocks; c += 2) {
+                    uint32_t x[2][16];
+                    tmem_ld16_async(s_addr + 16 * c, x[0]);
+                    tmem_ld16_async(s_addr + 16 * c + 16, x[1]);
+                    tmem_ld16_wait(x[0]);
+                    tmem_ld16_wait(x[1]);
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) x[c][i] = fmaf(x[c][i], f, -base), most = fmaxf(most, x[c][i]);
-                    } else {
+                    for (int d = 0; d < 2; ++d) {
+                        float top = -INFINITY;
+                        if (!masked) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            x[c][i] = t * kKeys + 16 * c + i < sees ? fmaf(x[c][i], f, -base) : -INFINITY;
-                            most = fmaxf(most, x[c][i]);
+                            for (int i = 0; i < 16; ++i) top = fmaxf(top, __uint_as_float(x[d][i]));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (t * kKeys + 16 * (c + d) + i < sees) top = fmaxf(top, __uint_as_float(x[d][i]));
                         }
+                        most = fmaxf(most, top * (cs * key_unit[c + d]));
+                        top_unit = max(top_unit, value_unit[c + d]);
                     }
                 }
-                const bool first = t == start;
-                if (first) o_unit = top_unit;
-                if (__any_sync(0xffffffffu, most > slack) || top_unit > o_unit) {
-                    float y = most, r = 1.f;
-                    if (slack != -INFINITY) y = fmaxf(y, 0.f), r = fast_exp2(-y);
-                    if (y != -INFINITY) {
-                        base += y, slack = kSlack;
-#pragma unroll
-                        for (int c = 0; c < kBlocks; ++c)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) x[c][i] -= y;
-                    }
-                    l *= r;
-                    if (top_unit > o_unit) r *= exp2f((float)(o_unit - top_unit)), o_unit = top_unit;
-                    if (!first) {                            // O in tensor memory, when the tile before is in it
-                        ok = warp_wait(smem_u32(&sh->o_done[b ^ 1]), ((g - 1) >> 1) & 1, abort_flag);
-                        if (!ok) break;
-                        tc_fence_after();
+                // the base and the unit of O of the tile before, and then of this one
+                float from = -INFINITY;
+                o_unit = -1000;
+                if (t > start) {
+                    ok = role_wait(smem_u32(&sh->based[quad]), (g - 1) & 1, abort_flag);
+                    if (!ok) break;
+                    from = sh->base[group ^ 1][r];
+                    o_unit = sh->o_unit[group ^ 1];
+                }
+                float now = from;
+                if (most > from + kSlack) now = most;        // also where nothing has been seen so far
+                const int now_unit = max(o_unit, top_unit);
+                sh->base[group][r] = now;
+                if (lane == 0) sh->o_unit[group] = now_unit;  // every warp of the group writes the same
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh->based[quad]));
+                if (base != now && base != -INFINITY) l *= fast_exp2(base - now);
+                base = now;
+                if (t > start && __any_sync(0xffffffffu, from != now || o_unit != now_unit)) {
+                    // O in tensor memory, when the tile before is in it
+                    const float f = (from == now || from == -INFINITY ? 1.f : fast_exp2(from - now)) * exp2f((float)(o_unit - now_unit));
+                    ok = role_wait(smem_u32(&sh->o_done[group ^ 1]), ((g - 1) >> 1) & 1, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
 #pragma unroll 1
-                        for (int i = 0; i < kD; i += 16) {
-                            uint32_t o[16];
-                            tmem_ld16_async(lane_tmem + kTmemO + i, o);
-                            tmem_ld16_wait(o);
+                    for (int i = 0; i < kD; i += 16) {
+                        uint32_t o[16];
+                        tmem_ld16_async(lane_tmem + kTmemO + i, o);
+                        tmem_ld16_wait(o);
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * r);
-                            tmem_st16_from<0>(lane_tmem + kTmemO + i, o);
-                        }
+                        for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * f);
+                        tmem_st16_from<0>(lane_tmem + kTmemO + i, o);
                     }
                 }
+                o_unit = now_unit;
+                if (g >= 2) {                                // PV has read the P that the group left last
+                    ok = role_wait(smem_u32(&sh->o_done[group]), ((g >> 1) - 1) & 1, abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                const float reference = now == -INFINITY ? 0.f : now;
+                // P is 2^lift times the probabilities of a block.  Below 2^-60 (a block whose values vanish beside others) that is not
+                // in the exponent: the sum of the probabilities is taken before.
+                uint32_t x[2][16];
+                tmem_ld16_async(s_addr, x[0]);
 #pragma unroll
                 for (int c = 0; c < kBlocks; ++c) {
-                    const float f = exp2f((float)(kHead + unit[c] - o_unit));
-                    uint32_t w[16];
-                    float s0 = 0.f, s1 = 0.f;
+                    uint32_t (&y)[16] = x[c & 1];
+                    tmem_ld16_wait(y);
+                    if (c + 1 < kBlocks) tmem_ld16_async(s_addr + 16 * (c + 1), x[(c + 1) & 1]);
+                    const int e = kHead + value_unit[c] - o_unit;
+                    const float lift = e < -60 ? 0.f : (float)e, f = cs * key_unit[c], add = lift - reference;
+                    const uint64_t f2 = pack_f2(f, f), add2 = pack_f2(add, add);
+                    uint64_t sum2 = 0;
+                    if (!masked && e >= -60) {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float p0 = fast_exp2(x[c][i]), p1 = fast_exp2(x[c][i + 1]);
-                        s0 += p0, s1 += p1;
-                        w[i >> 1] = pack_f16(p0 * f, p1 * f);
+                        for (int i = 0; i < 16; i += 2) {
+                            float p0, p1;
+                            unpack_f2(fma_f2(pack_f2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), f2, add2), p0, p1);
+                            p0 = fast_exp2(p0), p1 = fast_exp2(p1);
+                            sum2 = add_f2(sum2, pack_f2(p0, p1));
+                            y[i >> 1] = pack_f16(p0, p1);
+                        }
+                    } else {
+                        const int valid = sees - (t * kKeys + 16 * c);
+                        const float after = e < -60 ? exp2f((float)e) : 1.f;
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            const float p0 = i < valid ? fast_exp2(fmaf(__uint_as_float(y[i]), f, add)) : 0.f;
+                            const float p1 = i + 1 < valid ? fast_exp2(fmaf(__uint_as_float(y[i + 1]), f, add)) : 0.f;
+                            sum2 = add_f2(sum2, pack_f2(p0, p1));
+                            y[i >> 1] = pack_f16(p0 * after, p1 * after);
+                        }
                     }
-                    l += s0 + s1;
-                    tmem_st8_async(s_addr + 8 * c, w);
+                    float s0, s1;
+                    unpack_f2(sum2, s0, s1);
+                    l = fmaf(s0 + s1, __int_as_float((127 - (int)lift) << 23), l);
+                    tmem_st8_async(p_addr + 8 * c, y);
                 }
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready[b]));
+                if (lane == 0) mbar_arrive(smem_u32(&sh->p_ready[group]));
             }
             if (!ok) break;
+            // the last tile's base and unit, and the sum of both groups
+            float final_base = base;
+            {
+                const float theirs = exchange(base), sum = ok ? exchange(l) : 0.f;
+                if (!ok) break;
+                const bool last_is_mine = ((g - 1) & 1) == group;
+                final_base = last_is_mine ? base : theirs;
+                const float mine_f = base == final_base || base == -INFINITY ? 1.f : fast_exp2(base - final_base);
+                const float their_f = theirs == final_base || theirs == -INFINITY ? 1.f : fast_exp2(theirs - final_base);
+                l = l * mine_f + sum * their_f;
+                o_unit = sh->o_unit[(g - 1) & 1];
+            }
             // results, or a part of them
-            ok = warp_wait(smem_u32(&sh->o_done[(g - 1) & 1]), ((g - 1) >> 1) & 1, abort_flag);
+            ok = role_wait(smem_u32(&sh->o_done[(g - 1) & 1]), ((g - 1) >> 1) & 1, abort_flag);
             if (!ok) break;
             tc_fence_after();
             unsigned bad = 0;                                // groups of dims that a NaN reached
             if (sh->nan_unit[ordinal % kUnits] == ordinal + 1)
-                for (int r = max(start * kKeys, max(0, all_see)); r < min(sees, last * kKeys); ++r) {
-                    const int block = r / kBlockRows, col = a.blocks_per_page.quotient(block), page = pv.table[(size_t)p.request * pv.table_cols + col];
+                for (int row = max(start * kKeys, max(0, all_see)); row < min(sees, last * kKeys); ++row) {
+                    const int block = row / kBlockRows, col = a.blocks_per_page.quotient(block), page = pv.table[(size_t)p.request * pv.table_cols + col];
                     if ((unsigned)page >= (unsigned)pv.n_pages) continue;
                     const uint2 s = *reinterpret_cast<const uint2*>(
                         a.kv4 + (size_t)p.layer * a.kv4_layer_stride +
-                        (((size_t)page * a.n_kv_heads + head) * a.blocks_per_page.d + a.blocks_per_page.remainder(block)) * kBlockBytes + value_scale_at<kD>(r % kBlockRows));
+                        (((size_t)page * a.n_kv_heads + head) * a.blocks_per_page.d + a.blocks_per_page.remainder(block)) * kBlockBytes + value_scale_at<kD>(row % kBlockRows));
                     const float v[4] = {bf16_low(s.x), bf16_high(s.x), bf16_low(s.y), bf16_high(s.y)};
 #pragma unroll
                     for (int j = 0; j < 4; ++j) bad |= v[j] != v[j] ? 1u << j : 0u;
                 }
             const bool begins = p.at <= cost, whole = begins && p.end() == p.length;
             const int slot = 2 * share + (begins ? 1 : 0);
-            const float m = slack == -INFINITY ? -INFINITY : base, o_scale = exp2f((float)(o_unit - kHead));
+            const float m = final_base, o_scale = exp2f((float)(o_unit - kHead));
             const float f = !whole ? o_scale : l == 0.f ? 0.f : o_scale / l;
             __nv_bfloat16* out = out_row<__nv_bfloat16, kD>(a, p.layer, p.request, head, min(column, a.columns - 1));
-            float* part = a.part_o + ((size_t)slot * kTcColumns + tid) * kD;
+            float* part = a.part_o + ((size_t)slot * kTcColumns + r) * kD;
 #pragma unroll 1
-            for (int i = 0; i < kD; i += 16) {
+            for (int i = group * (kD / 2); i < (group + 1) * (kD / 2); i += 16) {
                 uint32_t o[16];
                 tmem_ld16_async(lane_tmem + kTmemO + i, o);
                 tmem_ld16_wait(o);
@@ -451,11 +559,13 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                     for (int j = 0; j < 16; j += 4) *reinterpret_cast<uint4*>(part + i + j) = make_uint4(o[j], o[j + 1], o[j + 2], o[j + 3]);
                 }
             }
-            if (whole) {
-                if (real) store_lse(a, pv.n_requests, p.layer, p.request, head, column, m, l);
-            } else {
-                a.part_ml[(size_t)slot * 2 * kTcColumns + tid] = m;
-                a.part_ml[(size_t)slot * 2 * kTcColumns + kTcColumns + tid] = l;
+            if (group == 0) {
+                if (whole) {
+                    if (real) store_lse(a, pv.n_requests, p.layer, p.request, head, column, m, l);
+                } else {
+                    a.part_ml[(size_t)slot * 2 * kTcColumns + r] = m;
+                    a.part_ml[(size_t)slot * 2 * kTcColumns + kTcColumns + r] = l;
+                }
             }
             if (tid == 0 && begins && (!whole || a.marks_by_unit)) {
                 const long long more = p.length - p.end();
@@ -487,13 +597,18 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
 
 }  // namespace
 
-bool kv4_attn_tc_supported(const cf_geom* g, int columns) {
-#ifndef TCMIN
-#define TCMIN 32
-#endif
-    return g->dtype == CF_BF16 && g->head_dim == kD && columns > TCMIN;
+// From 56 query columns on, and eight units: below, the kernel of cf_kv4_attn.cu is faster, whose units are 16 columns.  Measured
+// (that one / this one, us, 48, 64 and 128 columns): 4 requests of 4-16 K rows, 32/4 heads 30.1 / 30.9, 35.4 / 31.4, 59.2 / 33.8; 32 of
+// 200-2000 rows 29.8 / 35.3, 35.9 / 36.2, 61.6 / 40.0; one of 8000 rows (four units) 15.4 / 20.1, 16.4 / 20.8, 21.3 / 23.1; one of 500
+// 11.4 / 16.6, 12.1 / 16.9, 12.6 / 18.6.
+bool kv4_attn_tc_supported(const cf_geom* g, int columns, double units) {
+    return g->dtype == CF_BF16 && g->head_dim == kD && columns > 56 && units >= 8;
 }
 
+// 24 query tokens over 4 requests of 4-16 K rows, 28/4 heads (168 columns): 49 us with the join of the parts, 77 by the kernel of
+// cf_kv4_attn.cu; 13.7 GFLOP, 0.17 of the measured peak.  A tile of 64 keys takes 1900 cycles, of which its products are 512: what
+// bounds it is the chain of a softmax group (two reads of S, three waits, 64 exponentials that share the unit with the other
+// group's), with 0.4 of the issue slots, the ALUs (conversions) and the unit for exponentials busy.
 int launch_kv4_attn_tc(const Kv4Args& a, const PagesView& pv, cudaStream_t stream) {
     static PerDeviceOnce once;
     const int rc = configure_smem_once(once, kv4_attn_tc_kernel, kTcSmem);

@@ -494,3 +494,79 @@ def test_many_queries_and_numbers_that_are_not_finite():
     out, lse = _attend(geom, pages, pool, q)
     want[0, 10:] = True
     assert torch.equal(torch.isnan(out[0]).cpu(), want) and torch.equal(torch.isnan(lse[0, 0]).cpu(), want[0, :, :, 0].T)
+
+
+@pytest.mark.parametrize("hq,hkv,lengths,page_rows,q_len,layers", [
+    (12, 2, [64, 1, 200, 63], 64, 16, 1), (4, 4, [500, 33], 48, 57, 2), (8, 1, [1500, 0, 17], 80, 47, 1), (28, 4, [40 * i % 333 for i in range(40)], 16, 9, 1)],
+    ids=lambda x: str(x) if isinstance(x, int) else "%dx%d" % (len(x), max(x)))
+def test_attention_of_many_query_columns_in_eight_units(hq, hkv, lengths, page_rows, q_len, layers):
+    """Enough columns and units for the tensor-core kernel."""
+    test_attention_of_many_query_columns(hq, hkv, lengths, page_rows, q_len, layers)
+
+
+@pytest.mark.parametrize("q_scale,softmax_scale", [(1e-20, 1e19), (3e4, 3e-5), (60.0, 0.0), (1e30, 1e-31), (0.0, 0.0), (5.0, -0.2)])
+def test_many_columns_of_any_size(q_scale, softmax_scale):
+    geom = cf.make_geom(12, 2, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, 2, 128, [333, 50, 128, 7], 32, 1, seed=9)
+    q = (torch.randn((1, 4, 20, 12, 128), generator=torch.Generator().manual_seed(4)) * q_scale).to(torch.bfloat16).cuda()
+    out, lse = _attend(geom, pages, pool, q, softmax_scale)
+    _check_attention(geom, out, lse, q, kept, softmax_scale or 128 ** -0.5)
+
+
+def test_many_columns_over_keys_and_values_of_any_size():
+    """Scales that grow and shrink along a request, tile by tile and inside tiles: the units of blocks and of O, and their limits."""
+    geom = cf.make_geom(16, 4, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, _ = _filled(geom, 4, 128, [300, 300, 300], 16, 1, seed=2)
+    rows = torch.arange(300, device="cuda")
+    slots = torch.stack([pages.table[b, rows // 16].long() * 16 + rows % 16 for b in range(3)])
+    gen = torch.Generator().manual_seed(1)
+    k, v = torch.randn((1, 3, 300, 4, 128), generator=gen), torch.randn((1, 3, 300, 4, 128), generator=gen)
+    v[0, 0] *= 2.0 ** torch.linspace(-30, 10, 300)[:, None, None]
+    v[0, 1] *= 2.0 ** torch.linspace(10, -30, 300)[:, None, None]
+    v[0, 1, 150:] *= 2.0 ** -60
+    v[0, 2] *= 1e-30
+    k[0, 1] *= 2.0 ** torch.linspace(-12, 2, 300)[:, None, None]
+    k[0, 2, 100:116] *= 2.0 ** torch.linspace(-10, 3, 16)[:, None, None]
+    k, v = k.bfloat16(), v.bfloat16()
+    cf.cf_kv4_write(geom, pages.desc, pool, slots, k.cuda(), v.cuda())
+    kept = [[[P.numbers(*P.quantise(x[0, b].double().numpy())) for x in (k, v)] for b in range(3)]]
+    q = torch.randn((1, 3, 20, 16, 128), generator=gen).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    _check_attention(geom, out, lse, q, kept, 128 ** -0.5)
+
+
+def test_many_columns_and_numbers_that_are_not_finite():
+    geom = cf.make_geom(8, 4, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, 4, 128, [140, 40], 16, 1, seed=5)
+    k, v = torch.randn((1, 1, 4, 128)).bfloat16(), torch.randn((1, 1, 4, 128)).bfloat16()
+    v[..., 2, 70] = float("inf")
+    slot = int(pages.table[0, 130 // 16]) * 16 + 130 % 16
+    cf.cf_kv4_write(geom, pages.desc, pool, torch.tensor([slot], device="cuda"), k.cuda(), v.cuda())
+    q = torch.randn((1, 2, 30, 8, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    want = torch.zeros((2, 30, 8, 128), dtype=torch.bool)
+    want[0, 20:, 4:6, 64:96] = True                 # row 130 of 140 is seen by the last ten of thirty queries; kv head 2, a group of dims
+    assert torch.equal(torch.isnan(out[0]).cpu(), want) and torch.isfinite(lse).all()
+    k[..., 2, 3] = float("nan")
+    cf.cf_kv4_write(geom, pages.desc, pool, torch.tensor([slot], device="cuda"), k.cuda(), torch.zeros_like(v).cuda())
+    out, lse = _attend(geom, pages, pool, q)
+    want[0, 20:, 4:6] = True
+    assert torch.equal(torch.isnan(out[0]).cpu(), want) and torch.equal(torch.isnan(lse[0, 0]).cpu(), want[0, :, :, 0].T)
+
+
+def test_many_columns_captured_and_on_a_stream_of_its_own():
+    geom = cf.make_geom(32, 8, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, 8, 128, [700, 90], 16, 3, seed=6)
+    q = torch.randn((6, 2, 20, 32, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    wide = torch.full_like(q, 99.0)
+    work = torch.empty(cf.cf_kv4_attn_workspace_bytes(geom, pages.desc, 20, 3), dtype=torch.uint8, device="cuda")
+    lse = torch.zeros((3, 2, 32, 20), device="cuda")
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        cf.cf_kv4_attn(geom, pages.desc, pool, q[::2], wide[::2], work, lse=lse)
+        cf.cf_kv4_attn(geom, pages.desc, pool, q[::2], wide[::2], work, lse=lse)
+    graph.replay()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert (wide[1::2] == 99.0).all()
+    _check_attention(geom, wide[::2], lse, q[::2], kept, 128 ** -0.5)
