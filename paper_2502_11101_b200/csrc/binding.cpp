@@ -357,6 +357,9 @@ bool dense_layers(const at::Tensor& t) {
     return true;
 }
 
+// The calls below check what they are given: on the current device, whose stream they take.
+void require_here(const at::Tensor& t) { require(t.is_cuda() && t.get_device() == c10::cuda::current_device(), "a tensor on the current device is expected"); }
+
 NATIVE(pages_resize) {                             // pages, rows, extra_rows, slots, stream
     return guarded([&] {
         Args in(argv, argc);
@@ -369,6 +372,8 @@ NATIVE(pages_resize) {                             // pages, rows, extra_rows, s
         require(rows.scalar_type() == at::kInt && rows.is_contiguous() && rows.numel() == p->n_requests, "rows: int32, one per request");
         require(!slots || (slots->scalar_type() == at::kLong && slots->is_contiguous() && slots->numel() % p->n_requests == 0),
                 "slots: int64, as many for each request");
+        require_here(rows);
+        if (slots) require_here(*slots);
         const int64_t room = slots ? slots->numel() / p->n_requests : 0;
         require(room <= INT32_MAX, "slots: too many");
         const int32_t* rp = (const int32_t*)rows.data_ptr();
@@ -395,7 +400,8 @@ RowSpan row_span(const cf_geom* g, const at::Tensor& kv4, const at::Tensor& slot
     if (r.rows <= 1) r.row_stride = (int64_t)g->n_kv_heads * g->head_dim;
     require(r.rows <= INT32_MAX && r.layers <= INT32_MAX, "k and v: too many rows");
     require(slots.scalar_type() == at::kLong && slots.is_contiguous() && slots.numel() == r.rows, "slots: int64, one per row of a layer");
-    require(kv4.scalar_type() == at::kByte && kv4.size(0) == r.layers, "kv4: bytes of as many layers");
+    require(kv4.scalar_type() == at::kByte && kv4.dim() >= 1 && kv4.size(0) == r.layers && dense_layers(kv4), "kv4: bytes of as many layers, each dense");
+    for (const at::Tensor* t : {&kv4, &slots, &k, &v}) require_here(*t);
     return r;
 }
 
@@ -447,7 +453,9 @@ NATIVE(kv4_attn) {                                 // geom, pages, kv4, q, out, 
         require(q.size(1) == p->n_requests && q.size(3) == g->n_q_heads && q.size(4) == g->head_dim, "q: of other sizes than the geometry and the pages");
         require(!lse || (lse->scalar_type() == at::kFloat && lse->is_contiguous() && lse->numel() == q.numel() / g->head_dim),
                 "lse: fp32, one per query and head");
-        require(kv4.scalar_type() == at::kByte && kv4.size(0) == q.size(0), "kv4: bytes of as many layers");
+        require(kv4.scalar_type() == at::kByte && kv4.dim() >= 1 && kv4.size(0) == q.size(0) && dense_layers(kv4), "kv4: bytes of as many layers, each dense");
+        for (const at::Tensor* t : {&kv4, &q, &out, &ws}) require_here(*t);
+        if (lse) require_here(*lse);
         require(q.size(0) <= INT32_MAX && q.size(2) <= INT32_MAX, "q: too many layers or tokens");
         const int32_t n = (int32_t)q.size(0), tokens = (int32_t)q.size(2);
         const int64_t qs = q.stride(0), os = out.stride(0), ps = kv4.stride(0);

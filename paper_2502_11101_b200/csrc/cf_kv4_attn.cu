@@ -15,12 +15,20 @@
 // The running maximum is raised only when a logit lies more than 2^8 above it: fp16 has room for that, and the
 // test is one vote of the warp.
 //
-// A block of 16 rows (2304 bytes at head_dim 128) comes by one bulk copy into a ring that belongs to the warp: no barrier
-// between warps, and 129 KB in flight per SM.  The blocks of all units (layer, request, kv head, tile of query columns)
+// A step is two blocks of 16 rows (4608 bytes at head_dim 128), one bulk copy into a ring of two steps that belongs to the
+// warp: no barrier between warps, and up to 147 KB in flight per SM.  The steps of all units (layer, request, kv head, tile of query columns)
 // lie end to end on one line, which is cut into equal shares; lengths are device data, so every warp finds its place by
-// walking the requests' lengths.  A share belongs to a warp where there are many units, else to the eight warps of a CTA, which
-// take its blocks in turn and join their results in shared memory.  Units cut between shares leave parts in the workspace, which
+// walking the requests' lengths.  A share belongs to a warp where there are many units, else to the warps of a CTA, which
+// take its steps in turn and join their results in shared memory.  Units cut between shares leave parts in the workspace, which
 // kv4_merge_kernel joins.
+//
+// Measured (B200, a call with its merge, caches in HBM): 8 requests of 19-21.6 K rows, 32/32 heads, 122 us until the part
+// throttles (6.1 TB/s, 0.94 of the copy rate; 134 in a loop); 96 of 17-6001 rows, 28/4, 45 us (3.7 TB/s); three layers-batched ragged
+// requests, 32/8, 16.8 us; one of 1011 rows, 12/2, 8.7 us.  The loop issues 222 (few columns) and 282 instructions for 16 keys, 64 of
+// them conversions, at 0.57 and 0.52 per cycle and scheduler: that is what bounds grouped heads; few columns meet HBM.
+// What the steps of its making gave (8 long 32/32 / 96 of 28/4, us): 16 keys a step, selects under masks 171 / 69; those behind a
+// branch 162 / 68; 32 keys, shares weighed by units 148 / 51; a column per (query, group) 122 / -; four warps a CTA with 168
+// registers - / 47; shares of single warps - / 45.
 #include <algorithm>
 #include <climits>
 
@@ -234,7 +242,8 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
 #pragma unroll 1
     for (int i = 0; i < kStages; ++i) feeder.feed();
     unsigned taken = 0;                                      // steps that were waited for
-    bool given_up = false;
+    bool given_up = false;                                   // a wait ran out: no copies are issued any more, and none waited for
+    unsigned lost = 0;                                       // which copy did not come
     const uint32_t code_lane = g * (D / 2) + t * (D / 8);    // a lane's codes within the rows of its half, keys and values alike
     const uint32_t scale_lane = g * (D / 16) + (FEW ? 4 * t % (D / 16) : 0);
 
@@ -314,8 +323,8 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
 
         for (int step = start + first_step; step < last; step += stride) {
             const uint32_t stage = taken % kStages, blocks = ring + stage * kStepBlocks * kBytes;
-            if (!given_up && !tc::mbar_wait(bars + 8 * stage, taken / kStages & 1, &s_abort)) given_up = true;
-            if (!given_up) ++taken;
+            const bool came = given_up || tc::mbar_wait(bars + 8 * stage, taken / kStages & 1, &s_abort);
+            ++taken;
             // S^T of 32 keys: s[block][half][own column]
             float s[kStepBlocks][2][kOwn];
 #pragma unroll
@@ -426,7 +435,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                     }
                 }
             }
-            bool raise = false;
+            bool raise = !came;                              // one vote for what is rare
 #pragma unroll
             for (int c = 0; c < kOwn; ++c) raise |= fmaxf(fmaxf(s[0][0][c], s[0][1][c]), fmaxf(s[1][0][c], s[1][1][c])) > slack[c];
             uint32_t most = scale_limit;                     // scales order as integers
@@ -436,6 +445,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                 for (int i = 0; i < kScaleWords; ++i) most = __vmaxu2(most, __vmaxu2(ws[x][0][i], ws[x][1][i]));
             raise |= most != scale_limit;
             if (__any_sync(0xffffffffu, raise)) {
+                if (__any_sync(0xffffffffu, !came)) given_up = true, lost = taken - 1;
                 float vmax = 0.f;
 #pragma unroll
                 for (int x = 0; x < kStepBlocks; ++x)
@@ -626,9 +636,9 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
         }
     }
     if (given_up) {                                          // its copies in flight are given the time to end
-        for (; taken < feeder.issued; ++taken) {
+        for (; lost < feeder.issued; ++lost) {
             const long long t0 = clock64();
-            while (!tc::mbar_try_wait(bars + 8 * (taken % kStages), taken / kStages & 1) && clock64() - t0 < tc::kWaitLimitCycles) {}
+            while (!tc::mbar_try_wait(bars + 8 * (lost % kStages), lost / kStages & 1) && clock64() - t0 < tc::kWaitLimitCycles) {}
         }
         if (lane == 0) atomicCAS(pv.status, 0, CF_ERR_TIMEOUT);
     }

@@ -113,10 +113,21 @@ def run_stack(geom, batch, plan, workspace, q, k, v, out, score_accum, schedule,
     return code, 0
 
 
+def _require_here(*tensors):
+    """The calls below check what they are given: on the current device, whose stream they take."""
+    for t in tensors:
+        _require(t is None or (t.is_cuda and t.get_device() == torch.cuda.current_device()), "a tensor on the current device is expected")
+
+
+def _dense_layers(t):
+    return t.dim() >= 1 and (t.shape[0] == 0 or t[0].is_contiguous())
+
+
 def pages_resize(pages, rows, extra_rows, slots, stream):
     _require(rows.dtype == torch.int32 and rows.is_contiguous() and rows.numel() == pages.n_requests, "rows: int32, one per request")
     _require(slots is None or (slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() % pages.n_requests == 0),
              "slots: int64, as many for each request")
+    _require_here(rows, slots)
     return B.load_library().cf_pages_resize(_ref(pages), rows.data_ptr(), extra_rows, 0 if slots is None else slots.numel() // pages.n_requests,
                                             B._ptr(slots), B._stream(stream))
 
@@ -135,7 +146,8 @@ def _rows(geom, kv4, slots, k, v):
     if n <= 1:
         stride = geom.n_kv_heads * geom.head_dim
     _require(slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == n, "slots: int64, one per row of a layer")
-    _require(kv4.dtype == torch.uint8 and kv4.shape[0] == k.shape[0], "kv4: bytes of as many layers")
+    _require(kv4.dtype == torch.uint8 and kv4.shape[0] == k.shape[0] and _dense_layers(kv4), "kv4: bytes of as many layers, each dense")
+    _require_here(kv4, slots, k, v)
     return k.shape[0], n, k.stride(0), stride
 
 
@@ -157,6 +169,7 @@ def kv4_attn(geom, pages, kv4, q, out, workspace, lse, scale, stream):
     _require(q.element_size() == size and out.element_size() == size, "q and out: the storage type of the geometry")
     _require(q.shape[1] == pages.n_requests and q.shape[3] == geom.n_q_heads and q.shape[4] == geom.head_dim, "q: of other sizes than the geometry and the pages")
     _require(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == q.numel() // geom.head_dim), "lse: fp32, one per query and head")
-    _require(kv4.dtype == torch.uint8 and kv4.shape[0] == q.shape[0], "kv4: bytes of as many layers")
+    _require(kv4.dtype == torch.uint8 and kv4.shape[0] == q.shape[0] and _dense_layers(kv4), "kv4: bytes of as many layers, each dense")
+    _require_here(kv4, q, out, workspace, lse)
     return B.load_library().cf_kv4_attn(_ref(geom), _ref(pages), q.shape[0], q.shape[2], q.data_ptr(), q.stride(0), kv4.data_ptr(), kv4.stride(0),
                                         scale, out.data_ptr(), out.stride(0), B._ptr(lse), workspace.data_ptr(), _bytes(workspace), B._stream(stream))

@@ -570,3 +570,19 @@ def test_many_columns_captured_and_on_a_stream_of_its_own():
     torch.cuda.synchronize()
     assert (wide[1::2] == 99.0).all()
     _check_attention(geom, wide[::2], lse, q[::2], kept, 128 ** -0.5)
+
+
+def test_tensors_of_the_host_are_refused():
+    geom = cf.make_geom(2, 1, 64, torch.bfloat16, 4096, 1e4)
+    pages = Pages(1, 16, 2, 2)
+    rows, slots = torch.zeros(1, dtype=torch.int32), torch.zeros((1, 1), dtype=torch.int64)
+    pool = torch.zeros((1, cf.cf_kv4_layer_bytes(geom, pages.desc)), dtype=torch.uint8, device="cuda")
+    k = torch.zeros((1, 1, 1, 64), dtype=torch.bfloat16)
+    q = torch.zeros((1, 1, 1, 2, 64), dtype=torch.bfloat16)
+    work = torch.zeros(1 << 22, dtype=torch.uint8, device="cuda")
+    for call in (lambda: cf.cf_pages_resize(pages.desc, rows, 0, slots.cuda()), lambda: cf.cf_pages_resize(pages.desc, rows.cuda(), 0, slots),
+                 lambda: cf.cf_kv4_write(geom, pages.desc, pool, slots.cuda(), k, k), lambda: cf.cf_kv4_read(geom, pages.desc, pool, slots, k.cuda(), k.cuda()),
+                 lambda: cf.cf_kv4_write(geom, pages.desc, pool.cpu(), slots.cuda(), k.cuda(), k.cuda()),
+                 lambda: cf.cf_kv4_attn(geom, pages.desc, pool, q, q.cuda(), work), lambda: cf.cf_kv4_attn(geom, pages.desc, pool, q.cuda(), q.cuda(), work.cpu())):
+        with pytest.raises(AssertionError):
+            call()

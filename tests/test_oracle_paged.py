@@ -4,6 +4,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2502_11101_b200 as cf
 from oracle import paged_oracle as P
@@ -164,3 +165,31 @@ def test_calls_that_make_no_sense_are_refused(lib):
     for odd in (cf.make_geom(4, 2, 96, cf.CF_BF16, 4096, 1e4), cf.cf_geom(4, 2, 64, 7, 0, 4096, 1e4)):
         assert lib.cf_kv4_write(ref(odd), ref(pages), 1, 1, FAKE, FAKE, FAKE, 256, 256, FAKE, 0, None) == cf.CF_ERR_UNSUPPORTED
         assert lib.cf_kv4_attn(ref(odd), ref(pages), 1, 1, FAKE, 0, FAKE, 0, 0.0, FAKE, 0, None, FAKE, 1 << 40, None) == cf.CF_ERR_UNSUPPORTED
+
+
+def test_the_binding_refuses_other_shapes_types_and_devices():
+    """Before anything reaches the library; tensors of the host are among what is refused."""
+    from paper_2502_11101_b200 import marshal_ctypes as M
+    geom, pages = cf.make_geom(4, 2, 64, cf.CF_BF16, 4096, 1e4), _pages()
+    rows, slots = torch.zeros(3, dtype=torch.int32), torch.zeros((3, 5), dtype=torch.int64)
+    pool = torch.zeros((2, cf.cf_kv4_layer_bytes(geom, pages)), dtype=torch.uint8)
+    k = torch.zeros((2, 3, 5, 2, 64), dtype=torch.bfloat16)
+    q, work = torch.zeros((2, 3, 1, 4, 64), dtype=torch.bfloat16), torch.zeros(1 << 20, dtype=torch.uint8)
+    lse = torch.zeros((2, 3, 4, 1))
+    bad = [lambda: M.pages_resize(pages, rows, 0, slots, None), lambda: M.pages_resize(pages, rows.long(), 0, slots, None),
+           lambda: M.pages_resize(pages, rows[:2], 0, slots, None), lambda: M.pages_resize(pages, rows, 0, slots.int(), None),
+           lambda: M.pages_resize(pages, rows, 0, slots.flatten()[:14], None), lambda: M.pages_resize(pages, rows, 0, slots.T, None)]
+    for call in (M.kv4_write, M.kv4_read):
+        bad += [lambda c=call: c(geom, pages, pool, slots, k, k, None), lambda c=call: c(geom, pages, pool, slots, k.float(), k.float(), None),
+                lambda c=call: c(geom, pages, pool, slots, k, k[:, :, :4], None), lambda c=call: c(geom, pages, pool, slots[:2], k, k, None),
+                lambda c=call: c(geom, pages, pool[:1], slots, k, k, None), lambda c=call: c(geom, pages, pool.float(), slots, k, k, None),
+                lambda c=call: c(geom, pages, pool, slots, k.transpose(1, 2), k.transpose(1, 2), None),
+                lambda c=call: c(geom, pages, pool, slots, k[..., :32], k[..., :32], None), lambda c=call: c(geom, pages, pool, slots.int(), k, k, None)]
+    bad += [lambda: M.kv4_attn(geom, pages, pool, q, q.clone(), work, lse, 0.0, None), lambda: M.kv4_attn(geom, pages, pool, q[0], q[0], work, lse, 0.0, None),
+            lambda: M.kv4_attn(geom, pages, pool, q, q.float(), work, lse, 0.0, None), lambda: M.kv4_attn(geom, pages, pool, q[:, :2], q[:, :2], work, None, 0.0, None),
+            lambda: M.kv4_attn(geom, pages, pool[:1], q, q, work, lse, 0.0, None), lambda: M.kv4_attn(geom, pages, pool, q, q, work, lse[:1], 0.0, None),
+            lambda: M.kv4_attn(geom, pages, pool, q, q, work, lse.double(), 0.0, None)]
+    for i, call in enumerate(bad):
+        with pytest.raises(AssertionError):
+            call()
+            pytest.fail("call %d was not refused" % i)
