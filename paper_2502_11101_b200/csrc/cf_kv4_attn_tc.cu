@@ -1,5 +1,5 @@
-// Attention of many query columns over the 4-bit pages by the tensor cores (cf_kv4_attn where a kv head has more query columns,
-// query heads times tokens, than a few; bf16 storage, head_dim 128): a follow-up question over cached documents, or the
+// Attention of many query columns over the 4-bit pages by the tensor cores (cf_kv4_attn from 56 query columns of a kv head on,
+// query heads times tokens; bf16 storage, head_dim 128): a follow-up question over cached documents, or the
 // verification of drafted tokens.
 //
 // A unit is 128 query columns of a (layer, request, kv head) and the request's rows, 64 at a time.  Roles of a CTA:
@@ -10,9 +10,9 @@
 //   warp 16     MMA issue, the warp converged and one lane elected
 //   warp 17     copies of the pool's blocks
 // S = Q K^T with the queries as the A operand in tensor memory, O += P V with P as the A operand, there too; four S buffers and two
-// of P, so that QK^T runs two tiles ahead and neither group waits for it.  A group reads its tile's S twice, for the maximum and for the probabilities; what
-// probabilities are taken from (`base`) goes from tile to tile, so a group has to wait for the other's maximum, not for its
-// probabilities.  (One group with two S buffers 52 us, two threads to a column 51, two CTAs of one group per SM 58; this one: see
+// of P, so that QK^T runs two tiles ahead and neither group waits for it.  A group reads its tile's S twice, for the maximum and
+// for the probabilities; what probabilities are taken from (`base`) goes from tile to tile, so a group has to wait for the other's
+// maximum, not for its probabilities.  (One group with two S buffers 52 us, two threads to a column 51, two CTAs of one group per SM 58; this one: see
 // launch_kv4_attn_tc.)
 // Numbers: a code times its scale is ten bits, exact in fp16 as long as the scales of a block of 16 rows lie within 2^28 of each
 // other: a block is kept in units of 2^c, c chosen so that its largest scale comes to lie in [2^12, 2^13) (smaller ones lose last
