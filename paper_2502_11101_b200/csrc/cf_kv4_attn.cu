@@ -22,9 +22,11 @@
 // take its steps in turn and join their results in shared memory.  Units cut between shares leave parts in the workspace, which
 // kv4_merge_kernel joins.
 //
+// Short caches do without the line: a unit has a cluster of CTAs, joined over distributed shared memory (see cut_of).
+//
 // Measured (B200, a call with its merge, caches in HBM): 8 requests of 19-21.6 K rows, 32/32 heads, 122 us until the part
 // throttles (6.1 TB/s, 0.94 of the copy rate; 134 in a loop); 96 of 17-6001 rows, 28/4, 45 us (3.7 TB/s); three layers-batched ragged
-// requests, 32/8, 16.8 us; one of 1011 rows, 12/2, 8.7 us.  The loop issues 222 (few columns) and 282 instructions for 16 keys, 64 of
+// requests, 32/8, 16.8 us; one of 1011 rows, 12/2, 7.0 us.  The loop issues 222 (few columns) and 282 instructions for 16 keys, 64 of
 // them conversions, at 0.57 and 0.52 per cycle and scheduler: that is what bounds grouped heads; few columns meet HBM.
 // What the steps of its making gave (8 long 32/32 / 96 of 28/4, us): 16 keys a step, selects under masks 171 / 69; those behind a
 // branch 162 / 68; 32 keys, shares weighed by units 148 / 51; a column per (query, group) 122 / -; four warps a CTA with 168
@@ -57,6 +59,7 @@ constexpr int kMostCost = 32;                     // of a unit, in steps
 // the warps that have a share of their own, or the CTA that has one.
 constexpr int kLeastAlone = 4, kLeastTogether = 8;
 constexpr int kCostAlone = 3, kCostTogether = 16;
+constexpr int kClusterSteps = 6;                  // most steps of a warp where a cluster has a unit
 constexpr int kLeastTc = 8, kCostTc = 6;          // of the tensor-core kernel, in steps of its own
 
 // Warps of a CTA, and CTAs of an SM.  With few columns the loop fits 128 registers: 16 warps per SM; without, and with twice the
@@ -96,6 +99,18 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ uint32_t pack_f16_rest(float lo, float hi, uint32_t packed) {
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&packed));
     return pack_f16(lo - f.x, hi - f.y);
+}
+// Sixteen bytes, and four, of the shared memory of another CTA of the cluster, at the place that `p` has in this one's.
+__device__ __forceinline__ float4 cluster_load4(const float* p, int rank) {
+    float4 x;
+    asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %4, %5;\nld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [a];\n}"
+                 : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(smem_u32(p)), "r"(rank) : "memory");
+    return x;
+}
+__device__ __forceinline__ float cluster_load(const float* p, int rank) {
+    float x;
+    asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %1, %2;\nld.shared::cluster.f32 %0, [a];\n}" : "=f"(x) : "r"(smem_u32(p)), "r"(rank) : "memory");
+    return x;
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
     uint32_t x;
@@ -187,6 +202,19 @@ struct Feeder {
 
 template <typename T> struct IsF32 { static constexpr bool value = sizeof(T) == 4; };
 
+// A part of a column's dims, or the sum of several.
+struct Part {
+    float top, sum;
+    float4 x;
+    __device__ __forceinline__ void add(float m, float l, const float4& y) {
+        if (m == -INFINITY && l == 0.f) return;              // no key seen
+        const float to = fmaxf(top, m), f0 = top == to ? 1.f : exp2f(top - to), f1 = m == to || m == -INFINITY ? 1.f : exp2f(m - to);
+        sum = fmaf(sum, f0, l * f1);
+        x.x = fmaf(x.x, f0, y.x * f1), x.y = fmaf(x.y, f0, y.y * f1), x.z = fmaf(x.z, f0, y.z * f1), x.w = fmaf(x.w, f0, y.w * f1);
+        top = to;
+    }
+};
+
 // FEW: the query columns times the groups fit the eight columns of a matrix product, which then has a column per (query, group):
 // one chain of products for all groups, and one set of probabilities instead of one per group.
 template <typename T, int D, int NT, bool FEW>
@@ -208,6 +236,8 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
     float* s_m = s_o + kWarps * kCols * kOStride;            // [kWarps][kCols]
     float* s_l = s_m + kWarps * kCols;                       // [kWarps][kCols]
     unsigned long long* s_bars = reinterpret_cast<unsigned long long*>(s_l + kWarps * kCols);   // [kWarps][kStages]
+    float* s_part = reinterpret_cast<float*>(smem);          // over the ring, of a unit that a cluster shares: [kCols][D] and
+    float* s_part_ml = s_part + kCols * D;                   // [2][kCols]
     __shared__ Walk s_walk[kWarps];
     __shared__ int s_next[kWarps];
     __shared__ volatile int s_abort;
@@ -221,21 +251,35 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
     asm volatile("fence.proxy.async;" ::: "memory");         // what earlier kernels wrote is read by bulk copies
 
     const bool together = a.warps_per_share > 1;             // the CTA's warps share a share
+    const int n_cluster = (int)a.cluster.d;                  // CTAs that share a unit, 0 for shares of the line
     const int share = together ? (int)blockIdx.x : (int)blockIdx.x * kWarps + warp;
     const int cost = a.unit_cost;
     const Line line = {pv, a.n_kv_heads * (int)a.tiles.d, cost, pv.table_cols * pv.page_rows, kStepLog2};
-    const long long per_layer = line.length_of_layer(), total = per_layer * a.n_layers;
-    const long long size = max(a.least_share, (total + a.n_shares - 1) / a.n_shares);
-    const long long begin = share * size, mine = min(size, total - begin);
     const bool writer = lane == 0 && (!together || warp == 0);
-    if (writer && !a.marks_by_unit) a.marks[share] = make_int4(0, 0, 0, 0);
-    if (share == 0 && (!together || warp == 0))
-        for (int b = lane; b < pv.n_requests; b += 32)
-            if (pv.rows[b] < 0 || pv.rows[b] > line.most) atomicCAS(pv.status, 0, CF_ERR_RANGE);
-    if (mine <= 0) return;                                   // a warp's or the whole CTA's, no barrier follows
-
-    Walk p = line.find(begin, mine, per_layer);
-    const int first_step = together ? warp : 0, stride = together ? kWarps : 1;
+    Walk p = {};
+    long long size = 0;
+    int first_step = together ? warp : 0, stride = together ? kWarps : 1, rank = 0;
+    if (n_cluster > 0) {
+        const int u = a.cluster.quotient((int)blockIdx.x), lb = a.units_of.quotient(u);
+        rank = (int)blockIdx.x - u * n_cluster;
+        first_step = rank * kWarps + warp, stride = n_cluster * kWarps;
+        p.unit = u - lb * line.units;
+        p.layer = a.requests.quotient(lb), p.request = lb - p.layer * pv.n_requests;
+        const int rows = pv.rows[p.request];
+        if ((rows < 0 || rows > line.most) && tid == 0) atomicCAS(pv.status, 0, CF_ERR_RANGE);
+        p.rows = min(max(rows, 0), line.most);
+        p.left = p.length = steps_of(p.rows, kStepLog2);
+    } else {
+        const long long per_layer = line.length_of_layer(), total = per_layer * a.n_layers;
+        size = max(a.least_share, (total + a.n_shares - 1) / a.n_shares);
+        const long long begin = share * size, mine = min(size, total - begin);
+        if (writer && !a.marks_by_unit) a.marks[share] = make_int4(0, 0, 0, 0);
+        if (share == 0 && (!together || warp == 0))
+            for (int b = lane; b < pv.n_requests; b += 32)
+                if (pv.rows[b] < 0 || pv.rows[b] > line.most) atomicCAS(pv.status, 0, CF_ERR_RANGE);
+        if (mine <= 0) return;                               // a warp's or the whole CTA's, no barrier follows
+        p = line.find(begin, mine, per_layer);
+    }
     const uint32_t ring = smem_u32(s_ring) + warp * kRing, bars = smem_u32(s_bars + warp * kStages);
     if (lane == 0) s_walk[warp] = p, s_next[warp] = p.first_step(cost) + first_step;
     Feeder<D> feeder = {pv, a, line, s_walk + warp, s_next + warp, first_step, stride, lane, 0, 0, nullptr, 0, ring, bars, 0u, false};
@@ -592,7 +636,10 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                     sum = fmaf(lw, k, sum);
                     x.x = fmaf(y.x, k, x.x), x.y = fmaf(y.y, k, x.y), x.z = fmaf(y.z, k, x.z), x.w = fmaf(y.w, k, x.w);
                 }
-                if (whole) {
+                if (n_cluster > 1) {                         // for the cluster, where the ring was
+                    *reinterpret_cast<float4*>(s_part + c * D + d) = x;
+                    if (d == 0) s_part_ml[c] = top, s_part_ml[kCols + c] = sum;
+                } else if (whole) {
                     if (column < a.columns) {
                         const float inv = sum == 0.f ? 0.f : 1.f / sum;
                         store4<T>(out_row<T, D>(a, p.layer, p.request, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
@@ -602,6 +649,22 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                     *reinterpret_cast<float4*>(a.part_o + ((size_t)slot * kCols + c) * D + d) = x;
                     if (d == 0) a.part_ml[(size_t)slot * 2 * kCols + c] = top, a.part_ml[(size_t)slot * 2 * kCols + kCols + c] = sum;
                 }
+            }
+            if (n_cluster > 1) {                             // the CTAs join their results, each a part of the dims
+                tc::cluster_sync();
+                for (int i = rank * kThreads + tid; i < kCols * (D / 4); i += n_cluster * kThreads) {
+                    const int c = i / (D / 4), d = i % (D / 4) * 4, column = col0 + c;
+                    Part x = {-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 4
+                    for (int k = 0; k < n_cluster; ++k)
+                        x.add(cluster_load(s_part_ml + c, k), cluster_load(s_part_ml + kCols + c, k), cluster_load4(s_part + c * D + d, k));
+                    if (column < a.columns) {
+                        const float inv = x.sum == 0.f ? 0.f : 1.f / x.sum;
+                        store4<T>(out_row<T, D>(a, p.layer, p.request, head, column) + d, x.x.x * inv, x.x.y * inv, x.x.z * inv, x.x.w * inv);
+                        if (d == 0) store_lse(a, pv.n_requests, p.layer, p.request, head, column, x.top, x.sum);
+                    }
+                }
+                tc::cluster_sync();                          // everyone has read
             }
             __syncthreads();
         } else {
@@ -629,7 +692,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                 }
             }
         }
-        if (writer && begins && (!whole || a.marks_by_unit)) {
+        if (n_cluster == 0 && writer && begins && (!whole || a.marks_by_unit)) {
             const long long more = p.length - p.end();        // of the unit in later shares
             const int lb = p.layer * pv.n_requests + p.request;
             a.marks[a.marks_by_unit ? lb * line.units + p.unit : share] = make_int4(whole ? 0 : 1 + (int)((more + size - 1) / size), share, lb, p.unit);
@@ -643,19 +706,6 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
         if (lane == 0) atomicCAS(pv.status, 0, CF_ERR_TIMEOUT);
     }
 }
-
-// A part of a column's dims, or the sum of several.
-struct Part {
-    float top, sum;
-    float4 x;
-    __device__ __forceinline__ void add(float m, float l, const float4& y) {
-        if (m == -INFINITY && l == 0.f) return;              // no key seen
-        const float to = fmaxf(top, m), f0 = top == to ? 1.f : exp2f(top - to), f1 = m == to || m == -INFINITY ? 1.f : exp2f(m - to);
-        sum = fmaf(sum, f0, l * f1);
-        x.x = fmaf(x.x, f0, y.x * f1), x.y = fmaf(x.y, f0, y.y * f1), x.z = fmaf(x.z, f0, y.z * f1), x.w = fmaf(x.w, f0, y.w * f1);
-        top = to;
-    }
-};
 
 constexpr int kAtOnce = 4;                        // parts whose loads are under way together
 
@@ -713,6 +763,7 @@ struct Cut {
     bool few;
     int tile, tiles, columns;                     // columns of a unit, units and columns of a kv head
     int warps, ctas, n_shares, warps_per_share;
+    int cluster;                                  // CTAs of a unit, 0: shares of the line
     int marks;                                    // units, or shares where they are fewer
     bool marks_by_unit;
 };
@@ -739,6 +790,21 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
     if (c.tc) {                                   // a share to a CTA, one to an SM
         c.ctas = c.n_shares = sm_count();
         c.warps_per_share = c.warps;
+    }
+    else {
+        // Short caches, by the room that the table has: units that fit the device at once, with few steps for a warp, have a cluster
+        // each, which joins its results without a second launch.  Measured (shares of the line / clusters, us): 12/2 heads, one
+        // request of 500, 1000, 2000, 4000, 8000 rows 9.0 / 6.8, 9.5 / 7.0, 9.3 / 8.0, 9.8 / 9.5, 10.0 / 12.3 (eight steps a warp); 28/4,
+        // eight requests of up to that 10.9 / 8.5, 11.3 / 8.7, 12.3 / 10.0, 13.1 / 12.4, 16.0 / 17.0; 32/32, eight: 13.3 / 8.3, 16.6 / 11.5,
+        // 22.7 / 19.2 (nine steps).
+        const double steps = ((double)p->table_cols * p->page_rows + kStepRows - 1) / kStepRows;
+        int cluster = 1;
+        while (cluster < 8 && cluster * c.warps < steps && 2 * units * cluster <= c.ctas) cluster *= 2;
+        if (units * cluster <= c.ctas && steps <= kClusterSteps * cluster * c.warps) {
+            c.cluster = cluster;
+            c.warps_per_share = c.warps;
+            c.ctas = (int)units * cluster;
+        }
     }
     c.marks_by_unit = units <= c.n_shares;
     c.marks = c.marks_by_unit ? (int)units : c.n_shares;
@@ -782,8 +848,9 @@ int launch_attn(const Kv4Args& a, const PagesView& pv, const Cut& c, cudaStream_
     const size_t smem = attn_smem(D, warps_of(FEW), tile_columns(D, NT, FEW));
     const int rc = configure_smem_once(once, kv4_attn_kernel<T, D, NT, FEW>, (int)smem);
     if (rc != CF_OK) return rc;
-    const int err = launch_chained(kv4_attn_kernel<T, D, NT, FEW>, dim3((unsigned)c.ctas), 32 * warps_of(FEW), smem, stream, a, pv);
-    return err != CF_OK ? err : launch_merge<T, D>(a, pv, c.tile, c.marks, stream);
+    const int err = launch_chained_clusters(kv4_attn_kernel<T, D, NT, FEW>, dim3((unsigned)c.ctas), 32 * warps_of(FEW), smem, (unsigned)std::max(1, c.cluster),
+                                            stream, a, pv);
+    return err != CF_OK || c.cluster > 0 ? err : launch_merge<T, D>(a, pv, c.tile, c.marks, stream);
 }
 
 template <typename T, int D>
@@ -845,6 +912,10 @@ int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, in
     a.least_share = c.warps_per_share == 1 ? kLeastAlone : kLeastTogether;
     a.unit_cost = c.warps_per_share == 1 ? kCostAlone : kCostTogether;
     if (c.tc) a.least_share = kLeastTc, a.unit_cost = kCostTc;
+    if (c.cluster > 0) {
+        a.unit_cost = 0;
+        a.cluster = Divisor(c.cluster), a.units_of = Divisor(geom->n_kv_heads * c.tiles), a.requests = Divisor(pages->n_requests);
+    }
     a.scale_log2 = scale * kLog2e;
     const PagesView pv = make_pages_view(pages);
     cudaStream_t s = static_cast<cudaStream_t>(stream);

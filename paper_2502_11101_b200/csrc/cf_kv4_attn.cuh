@@ -20,6 +20,7 @@ struct Kv4Args {
     Divisor group, tiles, blocks_per_page;
     int n_shares, warps_per_share, unit_cost;
     int marks_by_unit;                            // a mark for every unit, where there are fewer units than shares
+    Divisor cluster, units_of, requests;          // of short caches: CTAs of a unit (0: shares of the line); units of a (layer, request)
     long long least_share;
     float scale_log2;
 };

@@ -586,3 +586,36 @@ def test_tensors_of_the_host_are_refused():
                  lambda: cf.cf_kv4_attn(geom, pages.desc, pool, q, q.cuda(), work), lambda: cf.cf_kv4_attn(geom, pages.desc, pool, q.cuda(), q.cuda(), work.cpu())):
         with pytest.raises(AssertionError):
             call()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim,lengths,page_rows,q_len,layers", [CASES[i] for i in (0, 1, 2, 3, 4, 5, 6, 7, 9, 10, 11, 12, 13)],
+                         ids=lambda x: str(x) if not isinstance(x, list) else "%dx%d" % (len(x), max(x)))
+@pytest.mark.parametrize("cols", [3000, 0])
+def test_attention_with_room_for_long_requests(dtype, hq, hkv, dim, lengths, page_rows, q_len, layers, cols):
+    """A table with room for long requests has shares of the line where its columns only hold the rows there are has clusters."""
+    geom = cf.make_geom(hq, hkv, dim, DTYPES[dtype], 32768, 1e6)
+    need = max(1, -(-max(lengths) // page_rows))
+    pages, pool, kept = _filled(geom, hkv, dim, lengths, page_rows, layers, seed=len(lengths) + dim, cols=cols or need)
+    q = torch.randn((layers, len(lengths), q_len, hq, dim), generator=torch.Generator().manual_seed(4)).to(DTYPES[dtype]).cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    assert cf.cf_pages_status(pages.desc) == 0
+    _check_attention(geom, out, lse, q, kept, dim ** -0.5)
+
+
+@pytest.mark.parametrize("hq,hkv,rows,requests", [(4, 4, 60, 3), (4, 4, 500, 2), (12, 2, 250, 1), (12, 2, 5000, 1), (28, 4, 1000, 8), (28, 4, 90, 30)])
+def test_attention_by_clusters_of_every_size(hq, hkv, rows, requests):
+    geom = cf.make_geom(hq, hkv, 128, torch.bfloat16, 32768, 1e6)
+    lengths = [rows - i * rows // requests for i in range(requests)]
+    pages, pool, kept = _filled(geom, hkv, 128, lengths, 16, 1, seed=rows, cols=-(-rows // 16))
+    q = torch.randn((1, requests, 1, hq, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    _check_attention(geom, out, lse, q, kept, 128 ** -0.5)
+    graph = torch.cuda.CUDAGraph()
+    work = torch.empty(cf.cf_kv4_attn_workspace_bytes(geom, pages.desc, 1, 1), dtype=torch.uint8, device="cuda")
+    again = torch.zeros_like(out)
+    with torch.cuda.graph(graph):
+        for _ in range(3):
+            cf.cf_kv4_attn(geom, pages.desc, pool, q, again, work)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, again)
