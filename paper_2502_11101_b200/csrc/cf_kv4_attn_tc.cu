@@ -53,7 +53,7 @@ struct TcShared {
     volatile int abort_flag;
     float key_unit[kUnits][kBlocks];              // 2^c of a tile's blocks
     int value_unit[kUnits][kBlocks];              // c
-    int o_unit[2];                                // of O, by the last tiles of the two groups
+    int o_unit[2][4];                             // of O, by the last tiles of the two groups and, as `based`, by 32 query columns
     float base[2][kTcColumns];                    // of the last tiles of the two groups; -infinity: no key seen yet
     float row[2][2][kTcColumns];                  // by parity of the exchange and group
     volatile int nan_unit[kUnits];                // by ordinal: that + 1 where a unit has a NaN among the values that not all of its queries see
@@ -427,13 +427,13 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                     ok = role_wait(smem_u32(&sh->based[quad]), (g - 1) & 1, abort_flag);
                     if (!ok) break;
                     from = sh->base[group ^ 1][r];
-                    o_unit = sh->o_unit[group ^ 1];
+                    o_unit = sh->o_unit[group ^ 1][quad];
                 }
                 float now = from;
                 if (most > from + kSlack) now = most;        // also where nothing has been seen so far
                 const int now_unit = max(o_unit, top_unit);
                 sh->base[group][r] = now;
-                if (lane == 0) sh->o_unit[group] = now_unit;  // every warp of the group writes the same
+                if (lane == 0) sh->o_unit[group][quad] = now_unit;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&sh->based[quad]));
                 if (base != now && base != -INFINITY) l *= fast_exp2(base - now);
@@ -515,7 +515,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 const float mine_f = base == final_base || base == -INFINITY ? 1.f : fast_exp2(base - final_base);
                 const float their_f = theirs == final_base || theirs == -INFINITY ? 1.f : fast_exp2(theirs - final_base);
                 l = l * mine_f + sum * their_f;
-                o_unit = sh->o_unit[(g - 1) & 1];
+                o_unit = sh->o_unit[(g - 1) & 1][quad];
             }
             // results, or a part of them
             ok = role_wait(smem_u32(&sh->o_done[(g - 1) & 1]), ((g - 1) >> 1) & 1, abort_flag);
