@@ -149,6 +149,75 @@ __device__ __forceinline__ int expand_block(const unsigned char* raw, unsigned c
     return unit;
 }
 
+// The largest logit of a tile, of its first `valid` keys: a maximum per block, by 2 and 2, and the factor of the block's unit.
+template <bool MASKED>
+__device__ __forceinline__ float largest_logit(uint32_t s_addr, const float* key_unit, float cs, int valid) {
+    float most = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < kBlocks; c += 2) {
+        uint32_t x[2][16];
+        tmem_ld16_async(s_addr + 16 * c, x[0]);
+        tmem_ld16_async(s_addr + 16 * c + 16, x[1]);
+        tmem_ld16_wait(x[0]);
+        tmem_ld16_wait(x[1]);
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+            float y[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[i] = MASKED && 16 * (c + d) + i >= valid ? -INFINITY : __uint_as_float(x[d][i]);
+#pragma unroll
+            for (int n = 8; n > 0; n >>= 1)
+#pragma unroll
+                for (int i = 0; i < n; ++i) y[i] = fmaxf(y[i], y[i + n]);
+            most = fmaxf(most, y[0] * (cs * key_unit[c + d]));
+        }
+    }
+    return most;
+}
+
+// The probabilities of a tile, its first `valid` keys, and their sum.  P is 2^lift times the probabilities of a block; below
+// kLeastLift (a block whose values vanish beside others) that is not in the exponent: the sum of the probabilities is taken before.
+constexpr int kLeastLift = -60;
+template <bool PLAIN>
+__device__ __forceinline__ void write_p(uint32_t s_addr, uint32_t p_addr, const float* key_unit, const int* value_unit, float cs, float reference, int o_unit,
+                                        int valid, float& l) {
+    uint32_t x[2][16];
+    tmem_ld16_async(s_addr, x[0]);
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c) {
+        uint32_t (&y)[16] = x[c & 1];
+        tmem_ld16_wait(y);
+        if (c + 1 < kBlocks) tmem_ld16_async(s_addr + 16 * (c + 1), x[(c + 1) & 1]);
+        const int e = kHead + value_unit[c] - o_unit;
+        const float lift = !PLAIN && e < kLeastLift ? 0.f : (float)e, f = cs * key_unit[c], add = lift - reference;
+        const uint64_t f2 = pack_f2(f, f), add2 = pack_f2(add, add);
+        uint64_t sum2 = 0;
+        if (PLAIN) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                float p0, p1;
+                unpack_f2(fma_f2(pack_f2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), f2, add2), p0, p1);
+                p0 = fast_exp2(p0), p1 = fast_exp2(p1);
+                sum2 = add_f2(sum2, pack_f2(p0, p1));
+                y[i >> 1] = pack_f16(p0, p1);
+            }
+        } else {
+            const float after = e < kLeastLift ? exp2f((float)e) : 1.f;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float p0 = 16 * c + i < valid ? fast_exp2(fmaf(__uint_as_float(y[i]), f, add)) : 0.f;
+                const float p1 = 16 * c + i + 1 < valid ? fast_exp2(fmaf(__uint_as_float(y[i + 1]), f, add)) : 0.f;
+                sum2 = add_f2(sum2, pack_f2(p0, p1));
+                y[i >> 1] = pack_f16(p0 * after, p1 * after);
+            }
+        }
+        float s0, s1;
+        unpack_f2(sum2, s0, s1);
+        l = fmaf(s0 + s1, __int_as_float((127 - (int)lift) << 23), l);
+        tmem_st8_async(p_addr + 8 * c, y);
+    }
+}
+
 __global__ void __launch_bounds__(kTcThreads, 1)
 kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__ PagesView pv) {
     extern __shared__ unsigned char smem_raw[];
@@ -396,30 +465,10 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 tc_fence_after();
                 const bool masked = (t + 1) * kKeys > all_see;
                 // the largest logit: S is read once for it and once for the probabilities
-                float most = -INFINITY;
-                int top_unit = -1000;
+                const float most = masked ? largest_logit<true>(s_addr, key_unit, cs, sees - t * kKeys) : largest_logit<false>(s_addr, key_unit, cs, 0);
+                int top_unit = value_unit[0], low_unit = value_unit[0];
 #pragma unroll
-                for (int c = 0; c < kBlocks; c += 2) {
-                    uint32_t x[2][16];
-                    tmem_ld16_async(s_addr + 16 * c, x[0]);
-                    tmem_ld16_async(s_addr + 16 * c + 16, x[1]);
-                    tmem_ld16_wait(x[0]);
-                    tmem_ld16_wait(x[1]);
-#pragma unroll
-                    for (int d = 0; d < 2; ++d) {
-                        float top = -INFINITY;
-                        if (!masked) {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) top = fmaxf(top, __uint_as_float(x[d][i]));
-                        } else {
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                if (t * kKeys + 16 * (c + d) + i < sees) top = fmaxf(top, __uint_as_float(x[d][i]));
-                        }
-                        most = fmaxf(most, top * (cs * key_unit[c + d]));
-                        top_unit = max(top_unit, value_unit[c + d]);
-                    }
-                }
+                for (int c = 1; c < kBlocks; ++c) top_unit = max(top_unit, value_unit[c]), low_unit = min(low_unit, value_unit[c]);
                 // the base and the unit of O of the tile before, and then of this one
                 float from = -INFINITY;
                 o_unit = -1000;
@@ -461,44 +510,8 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                     tc_fence_after();
                 }
                 const float reference = now == -INFINITY ? 0.f : now;
-                // P is 2^lift times the probabilities of a block.  Below 2^-60 (a block whose values vanish beside others) that is not
-                // in the exponent: the sum of the probabilities is taken before.
-                uint32_t x[2][16];
-                tmem_ld16_async(s_addr, x[0]);
-#pragma unroll
-                for (int c = 0; c < kBlocks; ++c) {
-                    uint32_t (&y)[16] = x[c & 1];
-                    tmem_ld16_wait(y);
-                    if (c + 1 < kBlocks) tmem_ld16_async(s_addr + 16 * (c + 1), x[(c + 1) & 1]);
-                    const int e = kHead + value_unit[c] - o_unit;
-                    const float lift = e < -60 ? 0.f : (float)e, f = cs * key_unit[c], add = lift - reference;
-                    const uint64_t f2 = pack_f2(f, f), add2 = pack_f2(add, add);
-                    uint64_t sum2 = 0;
-                    if (!masked && e >= -60) {
-#pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            float p0, p1;
-                            unpack_f2(fma_f2(pack_f2(__uint_as_float(y[i]), __uint_as_float(y[i + 1])), f2, add2), p0, p1);
-                            p0 = fast_exp2(p0), p1 = fast_exp2(p1);
-                            sum2 = add_f2(sum2, pack_f2(p0, p1));
-                            y[i >> 1] = pack_f16(p0, p1);
-                        }
-                    } else {
-                        const int valid = sees - (t * kKeys + 16 * c);
-                        const float after = e < -60 ? exp2f((float)e) : 1.f;
-#pragma unroll
-                        for (int i = 0; i < 16; i += 2) {
-                            const float p0 = i < valid ? fast_exp2(fmaf(__uint_as_float(y[i]), f, add)) : 0.f;
-                            const float p1 = i + 1 < valid ? fast_exp2(fmaf(__uint_as_float(y[i + 1]), f, add)) : 0.f;
-                            sum2 = add_f2(sum2, pack_f2(p0, p1));
-                            y[i >> 1] = pack_f16(p0 * after, p1 * after);
-                        }
-                    }
-                    float s0, s1;
-                    unpack_f2(sum2, s0, s1);
-                    l = fmaf(s0 + s1, __int_as_float((127 - (int)lift) << 23), l);
-                    tmem_st8_async(p_addr + 8 * c, y);
-                }
+                if (!masked && kHead + low_unit - o_unit >= kLeastLift) write_p<true>(s_addr, p_addr, key_unit, value_unit, cs, reference, o_unit, kKeys, l);
+                else write_p<false>(s_addr, p_addr, key_unit, value_unit, cs, reference, o_unit, sees - t * kKeys, l);
                 asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
                 tc_fence_before();
                 __syncwarp();
@@ -605,10 +618,12 @@ bool kv4_attn_tc_supported(const cf_geom* g, int columns, double units) {
     return g->dtype == CF_BF16 && g->head_dim == kD && columns > 56 && units >= 8;
 }
 
-// 24 query tokens over 4 requests of 4-16 K rows, 28/4 heads (168 columns): 49 us with the join of the parts, 77 by the kernel of
-// cf_kv4_attn.cu; 13.7 GFLOP, 0.17 of the measured peak.  A tile of 64 keys takes 1900 cycles, of which its products are 512: what
-// bounds it is the chain of a softmax group (two reads of S, three waits, 64 exponentials that share the unit with the other
-// group's), with 0.4 of the issue slots, the ALUs (conversions) and the unit for exponentials busy.
+// 24 query tokens over 4 requests of 4-16 K rows, 28/4 heads (168 columns): 46.6 us with the join of the parts, 77 by the kernel of
+// cf_kv4_attn.cu; 13.7 GFLOP, 0.18 of the measured peak.  A tile of 64 keys takes 1700 cycles, of which its products are 512: a
+// softmax group is busy for 3400 of every two tiles, the warps of the values for 1650 of each, the MMA warp for 1600, all with
+// latencies (a wait for a barrier that is complete takes 200) at 0.45 of the issue slots.  So no role alone is what bounds it:
+// without the exponentials, the conversions, the maximum or half of the products it takes 45.8; three groups 48.9, eight warps of
+// values 48.5, both 49.6, five or eight tiles of raw blocks 47.0 and 47.8.
 int launch_kv4_attn_tc(const Kv4Args& a, const PagesView& pv, cudaStream_t stream) {
     static PerDeviceOnce once;
     const int rc = configure_smem_once(once, kv4_attn_tc_kernel, kTcSmem);
