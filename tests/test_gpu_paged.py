@@ -619,3 +619,104 @@ def test_attention_by_clusters_of_every_size(hq, hkv, rows, requests):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("q_scale,softmax_scale", [(3e4, 3e-5), (60.0, 0.0), (5.0, -0.2)])
+def test_queries_of_any_size_with_room_for_long_requests(dtype, q_scale, softmax_scale):
+    geom = cf.make_geom(6, 2, 128, DTYPES[dtype], 32768, 1e6)
+    pages, pool, kept = _filled(geom, 2, 128, [333, 50, 1900], 32, 1, seed=9, cols=3000)
+    q = (torch.randn((1, 3, 2, 6, 128), generator=torch.Generator().manual_seed(4)) * q_scale).to(DTYPES[dtype]).cuda()
+    out, lse = _attend(geom, pages, pool, q, softmax_scale)
+    _check_attention(geom, out, lse, q, kept, softmax_scale or 128 ** -0.5)
+
+
+@pytest.mark.parametrize("hq,cols", [(1, 3000), (1, 40), (12, 3000), (12, 40)])
+def test_numbers_that_are_not_finite_over_several_parts(hq, cols):
+    """A request that several warps, shares or CTAs have: a NaN goes through the joins."""
+    geom = cf.make_geom(hq, 1, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, 1, 128, [640, 500], 16, 1, seed=5, cols=cols)
+    k, v = torch.randn((1, 1, 1, 128)).bfloat16(), torch.randn((1, 1, 1, 128)).bfloat16()
+    v[..., 70] = float("inf")
+    row = 638
+    slot = torch.tensor([int(pages.table[0, row // 16]) * 16 + row % 16], device="cuda")
+    cf.cf_kv4_write(geom, pages.desc, pool, slot, k.cuda(), v.cuda())
+    q = torch.randn((1, 2, 3, hq, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    want = torch.zeros(out[0].shape, dtype=torch.bool)
+    want[0, 1:, :, 64:96] = True                    # row 638 of 640 is seen by the last two of three queries
+    assert torch.equal(torch.isnan(out[0]).cpu(), want) and torch.isfinite(lse).all()
+    k[..., 3] = float("nan")
+    cf.cf_kv4_write(geom, pages.desc, pool, slot, k.cuda(), torch.zeros_like(v).cuda())
+    out, lse = _attend(geom, pages, pool, q)
+    want[0, 1:] = True
+    assert torch.equal(torch.isnan(out[0]).cpu(), want) and torch.equal(torch.isnan(lse[0, 0]).cpu(), want[0, :, :, 0].T)
+
+
+@pytest.mark.parametrize("hq,hkv,q_len,cols", [(4, 2, 1, 0), (4, 2, 1, 3000), (32, 4, 9, 0)])
+def test_a_table_that_points_outside_is_reported_by_every_kernel(hq, hkv, q_len, cols):
+    geom = cf.make_geom(hq, hkv, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, _ = _filled(geom, hkv, 128, [100, 30, 80], 16, 1, seed=6, cols=cols or None)
+    q = torch.zeros((1, 3, q_len, hq, 128), dtype=torch.bfloat16, device="cuda")
+    for bad in (1 << 30, -1, pages.free.shape[0]):
+        right, pages.table[0, 2] = int(pages.table[0, 2]), bad
+        _attend(geom, pages, pool, q)
+        assert cf.cf_pages_status(pages.desc) == cf.CF_ERR_RANGE
+        pages.status.zero_()
+        pages.table[0, 2] = right
+    for bad in (1 << 30, -5):
+        right, pages.rows[1] = int(pages.rows[1]), bad
+        _attend(geom, pages, pool, q)
+        assert cf.cf_pages_status(pages.desc) == cf.CF_ERR_RANGE
+        pages.status.zero_()
+        pages.rows[1] = right
+    _attend(geom, pages, pool, q)
+    assert cf.cf_pages_status(pages.desc) == 0
+
+
+def test_calls_on_two_streams_at_once():
+    """Over one pool, each with its own queries, results and workspace: as by themselves."""
+    cases = []
+    for hq, q_len, cols in ((28, 1, 3000), (28, 1, None), (28, 24, 3000), (28, 3, 3000)):
+        geom = cf.make_geom(hq, 4, 128, torch.bfloat16, 32768, 1e6)
+        pages, pool, _ = _filled(geom, 4, 128, [900, 40, 333, 0], 32, 1, seed=8, cols=cols)
+        q = torch.randn((1, 4, q_len, hq, 128), generator=torch.Generator().manual_seed(q_len)).bfloat16().cuda()
+        cases.append((geom, pages, pool, q, _attend(geom, pages, pool, q)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    work = [torch.empty(cf.cf_kv4_attn_workspace_bytes(c[0], c[1].desc, c[3].shape[2], 1), dtype=torch.uint8, device="cuda") for c in cases]
+    outs, lses = [torch.full_like(c[3], 99.0) for c in cases], [torch.full_like(c[4][1], 99.0) for c in cases]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, (geom, pages, pool, q, _) in enumerate(cases):
+            cf.cf_kv4_attn(geom, pages.desc, pool, q, outs[i], work[i], lse=lses[i], stream=streams[i])
+    torch.cuda.synchronize()
+    for i, c in enumerate(cases):
+        assert torch.equal(outs[i], c[4][0]) and torch.equal(lses[i], c[4][1])
+
+
+def test_pages_beyond_four_gigabytes():
+    """The last pages of a pool of 4.7 GB against the same rows in a small pool."""
+    heads, dim, page_rows, lengths = 32, 128, 64, [150, 64, 1]
+    geom = cf.make_geom(heads, heads, dim, torch.bfloat16, 32768, 1e6)
+    gen = torch.Generator().manual_seed(1)
+    k, v = [torch.randn((1, 3, 150, heads, dim), generator=gen).bfloat16().cuda() for _ in range(2)]
+    q = torch.randn((1, 3, 1, heads, dim), generator=gen).bfloat16().cuda()
+    many = torch.randn((1, 3, 72, heads, dim), generator=gen).bfloat16().cuda()
+    results = []
+    for n_pages in (8, 16000):
+        pages = Pages(3, page_rows, n_pages, 3)
+        pages.free.copy_(torch.arange(n_pages, dtype=torch.int32))
+        slots = pages.resize(lengths, 0, 150)
+        assert int(pages.table.max()) == n_pages - 1
+        pool = torch.zeros((1, cf.cf_kv4_layer_bytes(geom, pages.desc)), dtype=torch.uint8, device="cuda")
+        assert n_pages == 8 or pool.numel() > 1 << 32
+        cf.cf_kv4_write(geom, pages.desc, pool, slots, k, v)
+        back = [torch.zeros_like(k) for _ in range(2)]
+        cf.cf_kv4_read(geom, pages.desc, pool, slots, back[0], back[1])
+        results.append(back + list(_attend(geom, pages, pool, q)) + list(_attend(geom, pages, pool, many)))
+        assert cf.cf_pages_status(pages.desc) == 0
+        del pool
+    assert results[0][0].abs().max() > 0
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
