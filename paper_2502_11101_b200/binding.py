@@ -631,7 +631,7 @@ def make_pages(table: torch.Tensor, rows: torch.Tensor, free_pages: torch.Tensor
     """The pages of a batch of requests: int32 device tensors the caller keeps alive, `table` [B, columns], `rows` [B],
     `free_pages` [pages of the pool], `free_count` [1], `status` [1].  cf_pages_init sets them up."""
     for t in (table, rows, free_pages, free_count, status):
-        assert t.dtype == torch.int32 and t.is_contiguous() and t.device == table.device
+        assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.device == table.device
     assert table.dim() == 2 and rows.shape == (table.shape[0],) and free_count.numel() == 1 and status.numel() == 1
     return cf_pages(table.shape[0], page_rows, free_pages.numel(), table.shape[1], table.data_ptr(), rows.data_ptr(),
                     free_pages.data_ptr(), free_count.data_ptr(), status.data_ptr())

@@ -360,6 +360,14 @@ bool dense_layers(const at::Tensor& t) {
 // The calls below check what they are given: on the current device, whose stream they take.
 void require_here(const at::Tensor& t) { require(t.is_cuda() && t.get_device() == c10::cuda::current_device(), "a tensor on the current device is expected"); }
 
+bool of_storage_type(const cf_geom* g, const at::Tensor& t) { return t.scalar_type() == (g->dtype == CF_BF16 ? at::kBFloat16 : at::kFloat); }
+
+// A pool of `layers` layers for the pages, each dense.
+void require_pool(const cf_geom* g, const cf_pages* p, const at::Tensor& kv4, int64_t layers) {
+    require(kv4.scalar_type() == at::kByte && kv4.dim() >= 1 && kv4.size(0) == layers && dense_layers(kv4), "kv4: bytes of as many layers, each dense");
+    require(layers == 0 || (uint64_t)(kv4.numel() / layers) >= cf_kv4_layer_bytes(g, p), "kv4: fewer bytes than the pages have");
+}
+
 NATIVE(pages_resize) {                             // pages, rows, extra_rows, slots, stream
     return guarded([&] {
         Args in(argv, argc);
@@ -369,7 +377,7 @@ NATIVE(pages_resize) {                             // pages, rows, extra_rows, s
         const int32_t extra = in.i32();
         const at::Tensor* slots = in.maybe_tensor();
         void* s = in.stream();
-        require(rows.scalar_type() == at::kInt && rows.is_contiguous() && rows.numel() == p->n_requests, "rows: int32, one per request");
+        require(rows.scalar_type() == at::kInt && rows.is_contiguous() && rows.numel() == p->n_requests && p->n_requests > 0, "rows: int32, one per request");
         require(!slots || (slots->scalar_type() == at::kLong && slots->is_contiguous() && slots->numel() % p->n_requests == 0),
                 "slots: int64, as many for each request");
         require_here(rows);
@@ -386,10 +394,10 @@ NATIVE(pages_resize) {                             // pages, rows, extra_rows, s
 struct RowSpan {
     int64_t layers, rows, layer_stride, row_stride;
 };
-RowSpan row_span(const cf_geom* g, const at::Tensor& kv4, const at::Tensor& slots, const at::Tensor& k, const at::Tensor& v) {
-    const int64_t size = g->dtype == CF_BF16 ? 2 : 4, nd = k.dim();
+RowSpan row_span(const cf_geom* g, const cf_pages* p, const at::Tensor& kv4, const at::Tensor& slots, const at::Tensor& k, const at::Tensor& v) {
+    const int64_t nd = k.dim();
     require(nd >= 4 && k.sizes() == v.sizes() && k.strides() == v.strides(), "k and v: one shape and stride");
-    require((int64_t)k.element_size() == size && (int64_t)v.element_size() == size, "k and v: the storage type of the geometry");
+    require(of_storage_type(g, k) && of_storage_type(g, v), "k and v: the storage type of the geometry");
     require(k.size(nd - 2) == g->n_kv_heads && k.size(nd - 1) == g->head_dim, "k and v: [layers, rows ..., heads, dims]");
     require(k.stride(nd - 1) == 1 && k.stride(nd - 2) == g->head_dim, "k and v: a row is dense");
     RowSpan r = {k.size(0), 1, k.stride(0), k.stride(nd - 3)};
@@ -400,7 +408,7 @@ RowSpan row_span(const cf_geom* g, const at::Tensor& kv4, const at::Tensor& slot
     if (r.rows <= 1) r.row_stride = (int64_t)g->n_kv_heads * g->head_dim;
     require(r.rows <= INT32_MAX && r.layers <= INT32_MAX, "k and v: too many rows");
     require(slots.scalar_type() == at::kLong && slots.is_contiguous() && slots.numel() == r.rows, "slots: int64, one per row of a layer");
-    require(kv4.scalar_type() == at::kByte && kv4.dim() >= 1 && kv4.size(0) == r.layers && dense_layers(kv4), "kv4: bytes of as many layers, each dense");
+    require_pool(g, p, kv4, r.layers);
     for (const at::Tensor* t : {&kv4, &slots, &k, &v}) require_here(*t);
     return r;
 }
@@ -413,7 +421,7 @@ NATIVE(kv4_write) {                                // geom, pages, kv4, slots, k
         const cf_pages* p = in.structure<cf_pages>(bp);
         const at::Tensor &kv4 = in.tensor(), &slots = in.tensor(), &k = in.tensor(), &v = in.tensor();
         void* s = in.stream();
-        const RowSpan r = row_span(g, kv4, slots, k, v);
+        const RowSpan r = row_span(g, p, kv4, slots, k, v);
         const int64_t* sp = (const int64_t*)slots.data_ptr();
         void *kp = k.data_ptr(), *vp = v.data_ptr(), *pool = kv4.data_ptr();
         const int64_t ps = kv4.stride(0);
@@ -429,7 +437,7 @@ NATIVE(kv4_read) {                                 // geom, pages, kv4, slots, k
         const cf_pages* p = in.structure<cf_pages>(bp);
         const at::Tensor &kv4 = in.tensor(), &slots = in.tensor(), &k = in.tensor(), &v = in.tensor();
         void* s = in.stream();
-        const RowSpan r = row_span(g, kv4, slots, k, v);
+        const RowSpan r = row_span(g, p, kv4, slots, k, v);
         const int64_t* sp = (const int64_t*)slots.data_ptr();
         void *kp = k.data_ptr(), *vp = v.data_ptr(), *pool = kv4.data_ptr();
         const int64_t ps = kv4.stride(0);
@@ -447,13 +455,12 @@ NATIVE(kv4_attn) {                                 // geom, pages, kv4, q, out, 
         const at::Tensor* lse = in.maybe_tensor();
         const float scale = in.real();
         void* s = in.stream();
-        const int64_t size = g->dtype == CF_BF16 ? 2 : 4;
         require(q.dim() == 5 && out.sizes() == q.sizes() && dense_layers(q) && dense_layers(out), "q and out: [layers, requests, tokens, heads, dims]");
-        require((int64_t)q.element_size() == size && (int64_t)out.element_size() == size, "q and out: the storage type of the geometry");
+        require(of_storage_type(g, q) && of_storage_type(g, out), "q and out: the storage type of the geometry");
         require(q.size(1) == p->n_requests && q.size(3) == g->n_q_heads && q.size(4) == g->head_dim, "q: of other sizes than the geometry and the pages");
         require(!lse || (lse->scalar_type() == at::kFloat && lse->is_contiguous() && lse->numel() == q.numel() / g->head_dim),
                 "lse: fp32, one per query and head");
-        require(kv4.scalar_type() == at::kByte && kv4.dim() >= 1 && kv4.size(0) == q.size(0) && dense_layers(kv4), "kv4: bytes of as many layers, each dense");
+        require_pool(g, p, kv4, q.size(0));
         for (const at::Tensor* t : {&kv4, &q, &out, &ws}) require_here(*t);
         if (lse) require_here(*lse);
         require(q.size(0) <= INT32_MAX && q.size(2) <= INT32_MAX, "q: too many layers or tokens");

@@ -123,8 +123,18 @@ def _dense_layers(t):
     return t.dim() >= 1 and (t.shape[0] == 0 or t[0].is_contiguous())
 
 
+def _of_storage_type(geom, t):
+    return t.dtype == (torch.bfloat16 if geom.dtype == B.CF_BF16 else torch.float32)
+
+
+def _require_pool(geom, pages, kv4, layers):
+    """A pool of `layers` layers for the pages, each dense."""
+    _require(kv4.dtype == torch.uint8 and kv4.dim() >= 1 and kv4.shape[0] == layers and _dense_layers(kv4), "kv4: bytes of as many layers, each dense")
+    _require(layers == 0 or kv4.numel() // layers >= B.cf_kv4_layer_bytes(geom, pages), "kv4: fewer bytes than the pages have")
+
+
 def pages_resize(pages, rows, extra_rows, slots, stream):
-    _require(rows.dtype == torch.int32 and rows.is_contiguous() and rows.numel() == pages.n_requests, "rows: int32, one per request")
+    _require(rows.dtype == torch.int32 and rows.is_contiguous() and rows.numel() == pages.n_requests > 0, "rows: int32, one per request")
     _require(slots is None or (slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() % pages.n_requests == 0),
              "slots: int64, as many for each request")
     _require_here(rows, slots)
@@ -132,11 +142,10 @@ def pages_resize(pages, rows, extra_rows, slots, stream):
                                             B._ptr(slots), B._stream(stream))
 
 
-def _rows(geom, kv4, slots, k, v):
+def _rows(geom, pages, kv4, slots, k, v):
     """(layers, rows of a layer, layer stride, row stride) of k and v."""
-    size = 2 if geom.dtype == B.CF_BF16 else 4
     _require(k.dim() >= 4 and k.shape == v.shape and k.stride() == v.stride(), "k and v: one shape and stride")
-    _require(k.element_size() == size and v.element_size() == size, "k and v: the storage type of the geometry")
+    _require(_of_storage_type(geom, k) and _of_storage_type(geom, v), "k and v: the storage type of the geometry")
     _require(k.shape[-2] == geom.n_kv_heads and k.shape[-1] == geom.head_dim, "k and v: [layers, rows ..., heads, dims]")
     _require(k.stride(-1) == 1 and k.stride(-2) == geom.head_dim, "k and v: a row is dense")
     stride, n = k.stride(-3), 1
@@ -146,30 +155,29 @@ def _rows(geom, kv4, slots, k, v):
     if n <= 1:
         stride = geom.n_kv_heads * geom.head_dim
     _require(slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == n, "slots: int64, one per row of a layer")
-    _require(kv4.dtype == torch.uint8 and kv4.shape[0] == k.shape[0] and _dense_layers(kv4), "kv4: bytes of as many layers, each dense")
+    _require_pool(geom, pages, kv4, k.shape[0])
     _require_here(kv4, slots, k, v)
     return k.shape[0], n, k.stride(0), stride
 
 
 def kv4_write(geom, pages, kv4, slots, k, v, stream):
-    layers, n, layer_stride, stride = _rows(geom, kv4, slots, k, v)
+    layers, n, layer_stride, stride = _rows(geom, pages, kv4, slots, k, v)
     return B.load_library().cf_kv4_write(_ref(geom), _ref(pages), layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), layer_stride,
                                          stride, kv4.data_ptr(), kv4.stride(0), B._stream(stream))
 
 
 def kv4_read(geom, pages, kv4, slots, k, v, stream):
-    layers, n, layer_stride, stride = _rows(geom, kv4, slots, k, v)
+    layers, n, layer_stride, stride = _rows(geom, pages, kv4, slots, k, v)
     return B.load_library().cf_kv4_read(_ref(geom), _ref(pages), layers, n, slots.data_ptr(), kv4.data_ptr(), kv4.stride(0), k.data_ptr(),
                                         v.data_ptr(), layer_stride, stride, B._stream(stream))
 
 
 def kv4_attn(geom, pages, kv4, q, out, workspace, lse, scale, stream):
-    size = 2 if geom.dtype == B.CF_BF16 else 4
     _require(q.dim() == 5 and out.shape == q.shape and q[0].is_contiguous() and out[0].is_contiguous(), "q and out: [layers, requests, tokens, heads, dims]")
-    _require(q.element_size() == size and out.element_size() == size, "q and out: the storage type of the geometry")
+    _require(_of_storage_type(geom, q) and _of_storage_type(geom, out), "q and out: the storage type of the geometry")
     _require(q.shape[1] == pages.n_requests and q.shape[3] == geom.n_q_heads and q.shape[4] == geom.head_dim, "q: of other sizes than the geometry and the pages")
     _require(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == q.numel() // geom.head_dim), "lse: fp32, one per query and head")
-    _require(kv4.dtype == torch.uint8 and kv4.shape[0] == q.shape[0] and _dense_layers(kv4), "kv4: bytes of as many layers, each dense")
+    _require_pool(geom, pages, kv4, q.shape[0])
     _require_here(kv4, q, out, workspace, lse)
     return B.load_library().cf_kv4_attn(_ref(geom), _ref(pages), q.shape[0], q.shape[2], q.data_ptr(), q.stride(0), kv4.data_ptr(), kv4.stride(0),
                                         scale, out.data_ptr(), out.stride(0), B._ptr(lse), workspace.data_ptr(), _bytes(workspace), B._stream(stream))

@@ -720,3 +720,27 @@ def test_pages_beyond_four_gigabytes():
     assert results[0][0].abs().max() > 0
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("marshal", ["native", "ctypes"])
+def test_small_pools_other_types_and_no_requests_are_refused(marshal, monkeypatch):
+    if marshal == "ctypes":
+        monkeypatch.setattr(cf.binding, "_NATIVE", marshal_ctypes)
+    geom, pages = cf.make_geom(4, 2, 64, torch.bfloat16, 4096, 1e4), Pages(3, 16, 10, 4)
+    slots = torch.full((3, 5), -1, dtype=torch.int64, device="cuda")
+    layer = cf.cf_kv4_layer_bytes(geom, pages.desc)
+    pool, small = torch.zeros((2, layer), dtype=torch.uint8, device="cuda"), torch.zeros((2, layer - 16), dtype=torch.uint8, device="cuda")
+    k = torch.zeros((2, 3, 5, 2, 64), dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros((2, 3, 1, 4, 64), dtype=torch.bfloat16, device="cuda")
+    work = torch.zeros(cf.cf_kv4_attn_workspace_bytes(geom, pages.desc, 1, 2), dtype=torch.uint8, device="cuda")
+    none = cf.make_pages(torch.zeros((0, 4), dtype=torch.int32, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"), pages.free, pages.count,
+                         pages.status, 16)
+    for call in (lambda: cf.cf_kv4_write(geom, pages.desc, small, slots, k, k), lambda: cf.cf_kv4_read(geom, pages.desc, small, slots, k, k),
+                 lambda: cf.cf_kv4_write(geom, pages.desc, pool, slots, k.half(), k.half()), lambda: cf.cf_kv4_read(geom, pages.desc, pool, slots, k.half(), k.half()),
+                 lambda: cf.cf_kv4_attn(geom, pages.desc, small, q, q.clone(), work), lambda: cf.cf_kv4_attn(geom, pages.desc, pool, q.half(), q.half(), work),
+                 lambda: cf.cf_pages_resize(none, torch.zeros(0, dtype=torch.int32, device="cuda"), 0, torch.zeros((0, 1), dtype=torch.int64, device="cuda"))):
+        with pytest.raises(AssertionError):
+            call()
+    cf.cf_kv4_write(geom, pages.desc, pool, slots, k, k)
+    cf.cf_kv4_attn(geom, pages.desc, pool, q, q.clone(), work)
+    assert cf.cf_pages_status(pages.desc) == 0

@@ -193,3 +193,28 @@ def test_the_binding_refuses_other_shapes_types_and_devices():
         with pytest.raises(AssertionError):
             call()
             pytest.fail("call %d was not refused" % i)
+
+
+def test_the_binding_refuses_small_pools_other_types_and_no_requests():
+    """Each before the device of the tensors is looked at: the message says so."""
+    from paper_2502_11101_b200 import marshal_ctypes as M
+    geom, pages = cf.make_geom(4, 2, 64, cf.CF_BF16, 4096, 1e4), _pages()
+    slots, layer = torch.zeros((3, 5), dtype=torch.int64), cf.cf_kv4_layer_bytes(geom, pages)
+    pool, small = torch.zeros((2, layer), dtype=torch.uint8), torch.zeros((2, layer - 16), dtype=torch.uint8)
+    k, q = torch.zeros((2, 3, 5, 2, 64), dtype=torch.bfloat16), torch.zeros((2, 3, 1, 4, 64), dtype=torch.bfloat16)
+    work = torch.zeros(1 << 20, dtype=torch.uint8)
+    for call in (M.kv4_write, M.kv4_read):
+        with pytest.raises(AssertionError, match="fewer bytes"):
+            call(geom, pages, small, slots, k, k, None)
+        with pytest.raises(AssertionError, match="storage type"):
+            call(geom, pages, pool, slots, k.half(), k.half(), None)
+    with pytest.raises(AssertionError, match="fewer bytes"):
+        M.kv4_attn(geom, pages, small, q, q, work, None, 0.0, None)
+    with pytest.raises(AssertionError, match="storage type"):
+        M.kv4_attn(geom, pages, pool, q.half(), q.half(), work, None, 0.0, None)
+    none = _pages(n_requests=0)
+    with pytest.raises(AssertionError, match="one per request"):
+        M.pages_resize(none, torch.zeros(0, dtype=torch.int32), 0, torch.zeros((0, 1), dtype=torch.int64), None)
+    host = [torch.zeros(n, dtype=torch.int32) for n in ((3, 4), 3, 10, 1, 1)]
+    with pytest.raises(AssertionError):
+        cf.make_pages(*host, 16)
