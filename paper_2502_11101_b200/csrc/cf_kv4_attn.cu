@@ -207,8 +207,8 @@ struct Part {
     float top, sum;
     float4 x;
     __device__ __forceinline__ void add(float m, float l, const float4& y) {
-        if (m == -INFINITY && l == 0.f) return;              // no key seen
-        const float to = fmaxf(top, m), f0 = top == to ? 1.f : exp2f(top - to), f1 = m == to || m == -INFINITY ? 1.f : exp2f(m - to);
+        // without a key m is -infinity and the rest 0 (or, where it saw only NaN, NaN): times 0 or 1 that stays
+        const float to = fmaxf(top, m), f0 = top == to ? 1.f : exp2_fast(top - to), f1 = m == to ? 1.f : exp2_fast(m - to);
         sum = fmaf(sum, f0, l * f1);
         x.x = fmaf(x.x, f0, y.x * f1), x.y = fmaf(x.y, f0, y.y * f1), x.z = fmaf(x.z, f0, y.z * f1), x.w = fmaf(x.w, f0, y.w * f1);
         top = to;
@@ -271,7 +271,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
         p.left = p.length = steps_of(p.rows, kStepLog2);
     } else {
         const long long per_layer = line.length_of_layer(), total = per_layer * a.n_layers;
-        size = max(a.least_share, (total + a.n_shares - 1) / a.n_shares);
+        size = max(a.least_share, quotient_up(total, a.n_shares));
         const long long begin = share * size, mine = min(size, total - begin);
         if (writer && !a.marks_by_unit) a.marks[share] = make_int4(0, 0, 0, 0);
         if (share == 0 && (!together || warp == 0))
@@ -363,7 +363,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
         for (int c = 0; c < kOwn; ++c) base[c] = 0.f, slack[c] = -INFINITY, l[c] = 0.f;
         int exponent = kLeastExponent;                       // values are taken in units of 2^(exponent - kHead)
         uint32_t scale_limit = (uint32_t)(127 + exponent) * 0x00800080u;   // 2^exponent as bf16, twice
-        float scale_down = exp2f((float)(kHead - exponent));
+        float scale_down = power_of_two(kHead - exponent);
 
         for (int step = start + first_step; step < last; step += stride) {
             const uint32_t stage = taken % kStages, blocks = ring + stage * kStepBlocks * kBytes;
@@ -502,10 +502,10 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                 float f = 1.f;
                 if (vmax > bf16_low(scale_limit)) {
                     const int e = min((int)(__float_as_uint(vmax) >> 23) - 126, 127);
-                    f = exp2f((float)(exponent - e));
+                    f = exp2_fast((float)(exponent - e));
                     exponent = e;
                     scale_limit = (uint32_t)(127 + e) * 0x00800080u;
-                    scale_down = exp2f((float)(kHead - e));
+                    scale_down = power_of_two(kHead - e);
                 }
 #pragma unroll
                 for (int c = 0; c < kOwn; ++c) {
@@ -591,7 +591,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
         }
 
         // the unit is done, or as much of it as the share has
-        const float unit_scale = exp2f((float)(exponent - kHead));
+        const float unit_scale = power_of_two(exponent - kHead);
         float m[kOwn];
 #pragma unroll
         for (int c = 0; c < kOwn; ++c) {
@@ -631,8 +631,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                 for (int w = 0; w < kWarps; ++w) {
                     const float mw = s_m[w * kCols + c], lw = s_l[w * kCols + c];
                     const float4 y = *reinterpret_cast<const float4*>(s_o + (w * kCols + c) * kOStride + d);
-                    if (mw == -INFINITY && lw == 0.f) continue;          // a warp that saw no key
-                    const float k = mw == -INFINITY ? 1.f : exp2f(mw - top);     // (one that saw only NaN has no maximum)
+                    const float k = mw == top ? 1.f : exp2_fast(mw - top);       // a warp that saw no key has zeros
                     sum = fmaf(lw, k, sum);
                     x.x = fmaf(y.x, k, x.x), x.y = fmaf(y.y, k, x.y), x.z = fmaf(y.z, k, x.z), x.w = fmaf(y.w, k, x.w);
                 }
@@ -641,7 +640,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                     if (d == 0) s_part_ml[c] = top, s_part_ml[kCols + c] = sum;
                 } else if (whole) {
                     if (column < a.columns) {
-                        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                        const float inv = sum == 0.f ? 0.f : reciprocal(sum);
                         store4<T>(out_row<T, D>(a, p.layer, p.request, head, column) + d, x.x * inv, x.y * inv, x.z * inv, x.w * inv);
                         if (d == 0) store_lse(a, pv.n_requests, p.layer, p.request, head, column, top, sum);
                     }
@@ -659,7 +658,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                     for (int k = 0; k < n_cluster; ++k)
                         x.add(cluster_load(s_part_ml + c, k), cluster_load(s_part_ml + kCols + c, k), cluster_load4(s_part + c * D + d, k));
                     if (column < a.columns) {
-                        const float inv = x.sum == 0.f ? 0.f : 1.f / x.sum;
+                        const float inv = x.sum == 0.f ? 0.f : reciprocal(x.sum);
                         store4<T>(out_row<T, D>(a, p.layer, p.request, head, column) + d, x.x.x * inv, x.x.y * inv, x.x.z * inv, x.x.w * inv);
                         if (d == 0) store_lse(a, pv.n_requests, p.layer, p.request, head, column, x.top, x.sum);
                     }
@@ -673,7 +672,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
                 const int c = tile_column(i), column = col0 + c;
                 if (whole) {
                     if (column < a.columns) {
-                        const float f = l[i] == 0.f ? 0.f : unit_scale / l[i];
+                        const float f = l[i] == 0.f ? 0.f : unit_scale * reciprocal(l[i]);
                         T* row = out_row<T, D>(a, p.layer, p.request, head, column) + 4 * g;
 #pragma unroll
                         for (int j = 0; j < kGroups; ++j)
@@ -695,7 +694,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
         if (n_cluster == 0 && writer && begins && (!whole || a.marks_by_unit)) {
             const long long more = p.length - p.end();        // of the unit in later shares
             const int lb = p.layer * pv.n_requests + p.request;
-            a.marks[a.marks_by_unit ? lb * line.units + p.unit : share] = make_int4(whole ? 0 : 1 + (int)((more + size - 1) / size), share, lb, p.unit);
+            a.marks[a.marks_by_unit ? lb * line.units + p.unit : share] = make_int4(whole ? 0 : 1 + (int)quotient_up(more, size), share, lb, p.unit);
         }
     }
     if (given_up) {                                          // its copies in flight are given the time to end
@@ -749,7 +748,7 @@ kv4_merge_kernel(Kv4Args args, PagesView pv, Divisor requests, int tile, int col
                 x.add(y.top, y.sum, y.x);
             }
             const int layer = requests.quotient(mark.z), request = mark.z - layer * pv.n_requests;
-            const float inv = x.sum == 0.f ? 0.f : 1.f / x.sum;
+            const float inv = x.sum == 0.f ? 0.f : reciprocal(x.sum);
             store4<T>(out_row<T, D>(a, layer, request, head, column) + d, x.x.x * inv, x.x.y * inv, x.x.z * inv, x.x.w * inv);
             if (d == 0) store_lse(a, pv.n_requests, layer, request, head, column, x.top, x.sum);
         }

@@ -234,7 +234,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
     const int share = blockIdx.x, cost = a.unit_cost;
     const Line line = {pv, a.n_kv_heads * (int)a.tiles.d, cost, pv.table_cols * pv.page_rows, kTcStepLog2};
     const long long per_layer = line.length_of_layer(), total = per_layer * a.n_layers;
-    const long long size = max(a.least_share, (total + a.n_shares - 1) / a.n_shares);
+    const long long size = max(a.least_share, quotient_up(total, a.n_shares));
     const long long begin = share * size, mine = min(size, total - begin);
     if (tid == 0 && !a.marks_by_unit) a.marks[share] = make_int4(0, 0, 0, 0);
     if (share == 0 && warp == 0)
@@ -583,7 +583,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
             if (tid == 0 && begins && (!whole || a.marks_by_unit)) {
                 const long long more = p.length - p.end();
                 const int lb = p.layer * pv.n_requests + p.request;
-                a.marks[a.marks_by_unit ? lb * line.units + p.unit : share] = make_int4(whole ? 0 : 1 + (int)((more + size - 1) / size), share, lb, p.unit);
+                a.marks[a.marks_by_unit ? lb * line.units + p.unit : share] = make_int4(whole ? 0 : 1 + (int)quotient_up(more, size), share, lb, p.unit);
             }
             tc_fence_before();                               // O has been read when the next unit's queries arrive
             ++ordinal;
