@@ -25,8 +25,8 @@
 // Short caches do without the line: a unit has a cluster of CTAs, joined over distributed shared memory (see cut_of).
 //
 // Measured (B200, a call with its merge, caches in HBM): 8 requests of 19-21.6 K rows, 32/32 heads, 122 us until the part
-// throttles (6.1 TB/s, 0.94 of the copy rate; 134 in a loop); 96 of 17-6001 rows, 28/4, 45 us (3.7 TB/s); three layers-batched ragged
-// requests, 32/8, 16.8 us; one of 1011 rows, 12/2, 7.0 us.  The loop issues 222 (few columns) and 282 instructions for 16 keys, 64 of
+// throttles (6.1 TB/s, 0.94 of the copy rate; 134 in a loop); 96 of 17-6001 rows, 28/4, 44.5 us (3.7 TB/s); four layers of three ragged
+// requests, 32/8, 16.2 us; one of 1011 rows, 12/2, 6.2 us.  The loop issues 222 (few columns) and 282 instructions for 16 keys, 64 of
 // them conversions, at 0.57 and 0.52 per cycle and scheduler: that is what bounds grouped heads; few columns meet HBM.
 // What the steps of its making gave (8 long 32/32 / 96 of 28/4, us): 16 keys a step, selects under masks 171 / 69; those behind a
 // branch 162 / 68; 32 keys, shares weighed by units 148 / 51; a column per (query, group) 122 / -; four warps a CTA with 168
@@ -59,7 +59,8 @@ constexpr int kMostCost = 32;                     // of a unit, in steps
 // the warps that have a share of their own, or the CTA that has one.
 constexpr int kLeastAlone = 4, kLeastTogether = 8;
 constexpr int kCostAlone = 3, kCostTogether = 16;
-constexpr int kClusterSteps = 6;                  // most steps of a warp where a cluster has a unit
+constexpr int kMostCluster = 8;
+constexpr int kClusterSteps = 6, kClusterStepsFew = 9;     // most steps of a warp where a cluster has a unit; with few columns
 constexpr int kLeastTc = 8, kCostTc = 6;          // of the tensor-core kernel, in steps of its own
 
 // Warps of a CTA, and CTAs of an SM.  With few columns the loop fits 128 registers: 16 warps per SM; without, and with twice the
@@ -792,14 +793,15 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
     }
     else {
         // Short caches, by the room that the table has: units that fit the device at once, with few steps for a warp, have a cluster
-        // each, which joins its results without a second launch.  Measured (shares of the line / clusters, us): 12/2 heads, one
-        // request of 500, 1000, 2000, 4000, 8000 rows 9.0 / 6.8, 9.5 / 7.0, 9.3 / 8.0, 9.8 / 9.5, 10.0 / 12.3 (eight steps a warp); 28/4,
-        // eight requests of up to that 10.9 / 8.5, 11.3 / 8.7, 12.3 / 10.0, 13.1 / 12.4, 16.0 / 17.0; 32/32, eight: 13.3 / 8.3, 16.6 / 11.5,
-        // 22.7 / 19.2 (nine steps).
+        // each, which joins its results without a second launch.  Measured (shares of the line / clusters, us, lengths of half to all of
+        // the room): 12/2 heads, one request of 500, 1000, 2000, 4000, 8000 rows 8.2 / 6.2, 8.5 / 6.2, 8.7 / 7.1, 8.7 / 8.5, 9.0 / 11.5
+        // (eight steps a warp); 28/4, eight requests of up to that 10.1 / 7.8, 10.7 / 8.0, 11.6 / 9.2, 12.1 / 11.6, 15.1 / 16.2 (eight);
+        // a column a head, 32/32, one of 2000, 4000, 8000 10.6 / 7.9, 11.8 / 9.8, 15.0 / 12.9, two of 4000, 8000 13.3 / 12.0, 19.3 / 19.7
+        // (eight steps), four of 4000 20.1 / 19.7 (eight), eight of 1000, 2000, 4000 15.3 / 11.0, 21.4 / 18.9 (nine), 30.0 / 30.4 (sixteen).
         const double steps = ((double)p->table_cols * p->page_rows + kStepRows - 1) / kStepRows;
         int cluster = 1;
-        while (cluster < 8 && cluster * c.warps < steps && 2 * units * cluster <= c.ctas) cluster *= 2;
-        if (units * cluster <= c.ctas && steps <= kClusterSteps * cluster * c.warps) {
+        while (cluster < kMostCluster && cluster * c.warps < steps && 2 * units * cluster <= c.ctas) cluster *= 2;
+        if (units * cluster <= c.ctas && steps <= (c.few ? kClusterStepsFew : kClusterSteps) * cluster * c.warps) {
             c.cluster = cluster;
             c.warps_per_share = c.warps;
             c.ctas = (int)units * cluster;
