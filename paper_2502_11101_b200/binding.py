@@ -658,7 +658,8 @@ def cf_kv4_layer_bytes(geom: cf_geom, pages: cf_pages) -> int:
 def cf_kv4_write(geom: cf_geom, pages: cf_pages, kv4: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                  stream=None) -> None:
     """Rows k, v [n_layers, ..., Hkv, D] into `slots` (int64, one per row of a layer, negative: nowhere) of the pool kv4 (uint8
-    [n_layers, ...], a layer dense).  Rows may be padded; the dimensions between layers and heads lie one behind the other."""
+    [n_layers, ...], a layer dense).  Rows may be padded; the dimensions between layers and heads lie one behind the other, and one
+    of size 1 may have any stride."""
     _check(_native().kv4_write(geom, pages, kv4, slots, k, v, stream), "cf_kv4_write")
 
 

@@ -390,23 +390,33 @@ NATIVE(pages_resize) {                             // pages, rows, extra_rows, s
     });
 }
 
-// Rows of k and v for the calls on the 4-bit pool: [layers, rows ..., heads, dims], rows one behind the other.
+// Distance between layers, where there are several: a dimension of size 1 may have any stride, nobody steps along it.
+int64_t layer_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : 0; }
+
+// Rows of k or v for the calls on the 4-bit pool: [layers, rows ..., heads, dims], rows one behind the other, as far apart as the
+// innermost of their dimensions that has several.
 struct RowSpan {
     int64_t layers, rows, layer_stride, row_stride;
 };
-RowSpan row_span(const cf_geom* g, const cf_pages* p, const at::Tensor& kv4, const at::Tensor& slots, const at::Tensor& k, const at::Tensor& v) {
-    const int64_t nd = k.dim();
-    require(nd >= 4 && k.sizes() == v.sizes() && k.strides() == v.strides(), "k and v: one shape and stride");
-    require(of_storage_type(g, k) && of_storage_type(g, v), "k and v: the storage type of the geometry");
-    require(k.size(nd - 2) == g->n_kv_heads && k.size(nd - 1) == g->head_dim, "k and v: [layers, rows ..., heads, dims]");
-    require(k.stride(nd - 1) == 1 && k.stride(nd - 2) == g->head_dim, "k and v: a row is dense");
-    RowSpan r = {k.size(0), 1, k.stride(0), k.stride(nd - 3)};
+RowSpan rows_of(const cf_geom* g, const at::Tensor& t) {
+    const int64_t nd = t.dim();
+    require(nd >= 4 && t.size(nd - 2) == g->n_kv_heads && t.size(nd - 1) == g->head_dim, "k and v: [layers, rows ..., heads, dims]");
+    require(of_storage_type(g, t), "k and v: the storage type of the geometry");
+    require(t.stride(nd - 1) == 1 && (t.size(nd - 2) == 1 || t.stride(nd - 2) == g->head_dim), "k and v: a row is dense");
+    RowSpan r = {t.size(0), 1, layer_stride(t), (int64_t)g->n_kv_heads * g->head_dim};
     for (int64_t d = nd - 3; d > 0; --d) {
-        require(k.size(d) == 1 || k.stride(d) == r.row_stride * r.rows, "k and v: rows lie one behind the other");
-        r.rows *= k.size(d);
+        if (t.size(d) != 1 && t.numel() != 0) {
+            if (r.rows == 1) r.row_stride = t.stride(d);
+            require(t.stride(d) == r.row_stride * r.rows, "k and v: rows lie one behind the other");
+        }
+        r.rows *= t.size(d);
     }
-    if (r.rows <= 1) r.row_stride = (int64_t)g->n_kv_heads * g->head_dim;
     require(r.rows <= INT32_MAX && r.layers <= INT32_MAX, "k and v: too many rows");
+    return r;
+}
+RowSpan row_span(const cf_geom* g, const cf_pages* p, const at::Tensor& kv4, const at::Tensor& slots, const at::Tensor& k, const at::Tensor& v) {
+    const RowSpan r = rows_of(g, k), o = rows_of(g, v);
+    require(k.sizes() == v.sizes() && r.layer_stride == o.layer_stride && r.row_stride == o.row_stride, "k and v: one shape and stride");
     require(slots.scalar_type() == at::kLong && slots.is_contiguous() && slots.numel() == r.rows, "slots: int64, one per row of a layer");
     require_pool(g, p, kv4, r.layers);
     for (const at::Tensor* t : {&kv4, &slots, &k, &v}) require_here(*t);
@@ -424,7 +434,7 @@ NATIVE(kv4_write) {                                // geom, pages, kv4, slots, k
         const RowSpan r = row_span(g, p, kv4, slots, k, v);
         const int64_t* sp = (const int64_t*)slots.data_ptr();
         void *kp = k.data_ptr(), *vp = v.data_ptr(), *pool = kv4.data_ptr();
-        const int64_t ps = kv4.stride(0);
+        const int64_t ps = layer_stride(kv4);
         return call([&] { return cf_kv4_write(g, p, (int32_t)r.layers, (int32_t)r.rows, sp, kp, vp, r.layer_stride, r.row_stride, pool, ps, s); });
     });
 }
@@ -440,7 +450,7 @@ NATIVE(kv4_read) {                                 // geom, pages, kv4, slots, k
         const RowSpan r = row_span(g, p, kv4, slots, k, v);
         const int64_t* sp = (const int64_t*)slots.data_ptr();
         void *kp = k.data_ptr(), *vp = v.data_ptr(), *pool = kv4.data_ptr();
-        const int64_t ps = kv4.stride(0);
+        const int64_t ps = layer_stride(kv4);
         return call([&] { return cf_kv4_read(g, p, (int32_t)r.layers, (int32_t)r.rows, sp, pool, ps, kp, vp, r.layer_stride, r.row_stride, s); });
     });
 }
@@ -465,7 +475,7 @@ NATIVE(kv4_attn) {                                 // geom, pages, kv4, q, out, 
         if (lse) require_here(*lse);
         require(q.size(0) <= INT32_MAX && q.size(2) <= INT32_MAX, "q: too many layers or tokens");
         const int32_t n = (int32_t)q.size(0), tokens = (int32_t)q.size(2);
-        const int64_t qs = q.stride(0), os = out.stride(0), ps = kv4.stride(0);
+        const int64_t qs = layer_stride(q), os = layer_stride(out), ps = layer_stride(kv4);
         void *qp = q.data_ptr(), *op = out.data_ptr(), *pool = kv4.data_ptr(), *w = ws.data_ptr();
         float* lp = lse ? (float*)lse->data_ptr() : nullptr;
         const size_t wn = bytes_of(ws);

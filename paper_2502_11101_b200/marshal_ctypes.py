@@ -142,33 +142,45 @@ def pages_resize(pages, rows, extra_rows, slots, stream):
                                             B._ptr(slots), B._stream(stream))
 
 
+def _layer_stride(t):
+    """Distance between layers, where there are several: a dimension of size 1 may have any stride, nobody steps along it."""
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _rows_of(geom, t):
+    """(layers, rows of a layer, layer stride, row stride) of k or v: rows one behind the other, as far apart as the innermost of
+    their dimensions that has several."""
+    _require(t.dim() >= 4 and t.shape[-2] == geom.n_kv_heads and t.shape[-1] == geom.head_dim, "k and v: [layers, rows ..., heads, dims]")
+    _require(_of_storage_type(geom, t), "k and v: the storage type of the geometry")
+    _require(t.stride(-1) == 1 and (t.shape[-2] == 1 or t.stride(-2) == geom.head_dim), "k and v: a row is dense")
+    stride, n = geom.n_kv_heads * geom.head_dim, 1
+    for d in range(t.dim() - 3, 0, -1):
+        if t.shape[d] != 1 and t.numel() != 0:
+            if n == 1:
+                stride = t.stride(d)
+            _require(t.stride(d) == stride * n, "k and v: rows lie one behind the other")
+        n *= t.shape[d]
+    return t.shape[0], n, _layer_stride(t), stride
+
+
 def _rows(geom, pages, kv4, slots, k, v):
-    """(layers, rows of a layer, layer stride, row stride) of k and v."""
-    _require(k.dim() >= 4 and k.shape == v.shape and k.stride() == v.stride(), "k and v: one shape and stride")
-    _require(_of_storage_type(geom, k) and _of_storage_type(geom, v), "k and v: the storage type of the geometry")
-    _require(k.shape[-2] == geom.n_kv_heads and k.shape[-1] == geom.head_dim, "k and v: [layers, rows ..., heads, dims]")
-    _require(k.stride(-1) == 1 and k.stride(-2) == geom.head_dim, "k and v: a row is dense")
-    stride, n = k.stride(-3), 1
-    for d in range(k.dim() - 3, 0, -1):
-        _require(k.shape[d] == 1 or k.stride(d) == stride * n, "k and v: rows lie one behind the other")
-        n *= k.shape[d]
-    if n <= 1:
-        stride = geom.n_kv_heads * geom.head_dim
-    _require(slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == n, "slots: int64, one per row of a layer")
+    rows = _rows_of(geom, k)
+    _require(k.shape == v.shape and rows == _rows_of(geom, v), "k and v: one shape and stride")
+    _require(slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == rows[1], "slots: int64, one per row of a layer")
     _require_pool(geom, pages, kv4, k.shape[0])
     _require_here(kv4, slots, k, v)
-    return k.shape[0], n, k.stride(0), stride
+    return rows
 
 
 def kv4_write(geom, pages, kv4, slots, k, v, stream):
     layers, n, layer_stride, stride = _rows(geom, pages, kv4, slots, k, v)
     return B.load_library().cf_kv4_write(_ref(geom), _ref(pages), layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), layer_stride,
-                                         stride, kv4.data_ptr(), kv4.stride(0), B._stream(stream))
+                                         stride, kv4.data_ptr(), _layer_stride(kv4), B._stream(stream))
 
 
 def kv4_read(geom, pages, kv4, slots, k, v, stream):
     layers, n, layer_stride, stride = _rows(geom, pages, kv4, slots, k, v)
-    return B.load_library().cf_kv4_read(_ref(geom), _ref(pages), layers, n, slots.data_ptr(), kv4.data_ptr(), kv4.stride(0), k.data_ptr(),
+    return B.load_library().cf_kv4_read(_ref(geom), _ref(pages), layers, n, slots.data_ptr(), kv4.data_ptr(), _layer_stride(kv4), k.data_ptr(),
                                         v.data_ptr(), layer_stride, stride, B._stream(stream))
 
 
@@ -179,5 +191,5 @@ def kv4_attn(geom, pages, kv4, q, out, workspace, lse, scale, stream):
     _require(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == q.numel() // geom.head_dim), "lse: fp32, one per query and head")
     _require_pool(geom, pages, kv4, q.shape[0])
     _require_here(kv4, q, out, workspace, lse)
-    return B.load_library().cf_kv4_attn(_ref(geom), _ref(pages), q.shape[0], q.shape[2], q.data_ptr(), q.stride(0), kv4.data_ptr(), kv4.stride(0),
-                                        scale, out.data_ptr(), out.stride(0), B._ptr(lse), workspace.data_ptr(), _bytes(workspace), B._stream(stream))
+    return B.load_library().cf_kv4_attn(_ref(geom), _ref(pages), q.shape[0], q.shape[2], q.data_ptr(), _layer_stride(q), kv4.data_ptr(), _layer_stride(kv4),
+                                        scale, out.data_ptr(), _layer_stride(out), B._ptr(lse), workspace.data_ptr(), _bytes(workspace), B._stream(stream))

@@ -1,0 +1,119 @@
+"""Which rows the calls on the 4-bit pool take: layouts that torch gives to keys and values of one token, one layer, one head.  No
+GPU: tensors of the host pass the checks of layout and are refused for their device, or reach a library that only notes what it
+is given."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2502_11101_b200 as cf
+from paper_2502_11101_b200 import binding
+from paper_2502_11101_b200 import build as cf_build
+from paper_2502_11101_b200 import marshal_ctypes as M
+
+FAKE = 4096
+
+
+@pytest.fixture(scope="module")
+def lib():
+    cf_build.build()
+    return cf.load_library()
+
+
+def _pages(n_pages=10, page_rows=32):
+    return cf.cf_pages(3, page_rows, n_pages, 4, FAKE, FAKE, FAKE, FAKE, FAKE)
+
+
+def _cut(layers, requests, tokens, heads, dim, pad, dtype=torch.bfloat16):
+    """Keys and values cut out of a fused projection [layers, requests, tokens, K | V | rest]."""
+    n = heads * dim
+    wide = torch.zeros((layers, requests, tokens, 2 * n + pad), dtype=dtype)
+    return wide[..., :n].unflatten(-1, (heads, dim)), wide[..., n:2 * n].unflatten(-1, (heads, dim))
+
+
+class Noting:
+    """In place of the library: what a call is given."""
+
+    def __init__(self):
+        self.seen = []
+
+    def __getattr__(self, name):
+        if name == "cf_kv4_layer_bytes":
+            return lambda g, p: 0
+        return lambda *a: self.seen.append((name, a)) or 0
+
+
+# layers, requests, tokens, heads, dim, padding
+SHAPES = [(1, 8, 1, 4, 128, 8), (1, 1, 1, 4, 128, 8), (3, 8, 1, 4, 128, 64), (3, 1, 1, 2, 64, 8), (1, 1, 5, 2, 64, 16), (2, 7, 3, 1, 64, 8),
+          (2, 1, 4, 1, 128, 0), (1, 5, 1, 1, 64, 40)]
+
+
+@pytest.mark.parametrize("layers,requests,tokens,heads,dim,pad", SHAPES)
+def test_rows_cut_out_of_a_fused_projection(lib, monkeypatch, layers, requests, tokens, heads, dim, pad):
+    geom, pages = cf.make_geom(heads, heads, dim, torch.bfloat16, 4096, 1e4), _pages()
+    k, v = _cut(layers, requests, tokens, heads, dim, pad)
+    pool = torch.zeros((layers, cf.cf_kv4_layer_bytes(geom, pages)), dtype=torch.uint8)
+    slots = torch.zeros((requests, tokens), dtype=torch.int64)
+    row = 2 * heads * dim + pad
+    native = binding._load_native(cf_build.NATIVE_PATH)
+    for module in (M, native):
+        for call in (module.kv4_write, module.kv4_read):
+            with pytest.raises(AssertionError, match="current device"):      # the layout is taken, the host's tensors are not
+                call(geom, pages, pool, slots, k, v, 0)
+    note = Noting()
+    monkeypatch.setattr(M, "_require_here", lambda *t: None)
+    monkeypatch.setattr(binding, "load_library", lambda: note)
+    monkeypatch.setattr(binding, "_stream", lambda s: None)
+    for call in (M.kv4_write, M.kv4_read):
+        call(geom, pages, pool, slots, k, v, None)
+    (_, w), (_, r) = note.seen
+    n = requests * tokens
+    apart = row if n > 1 else heads * dim
+    between = n * row if layers > 1 else 0
+    assert w[2:9] == (layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), between, apart)
+    assert r[2:5] == (layers, n, slots.data_ptr()) and r[9:11] == (between, apart)
+
+
+@pytest.mark.parametrize("module", ["native", "ctypes"])
+def test_a_dimension_of_one_may_have_any_stride(lib, module):
+    """Layers, rows and heads of which there is one."""
+    module = binding._load_native(cf_build.NATIVE_PATH) if module == "native" else M
+    geom, pages = cf.make_geom(1, 1, 64, torch.bfloat16, 4096, 1e4), _pages()
+    base = torch.zeros(4096, dtype=torch.bfloat16)
+    pool = torch.zeros(1 << 20, dtype=torch.uint8).as_strided((1, cf.cf_kv4_layer_bytes(geom, pages)), (3, 1))
+    slots = torch.zeros(6, dtype=torch.int64)
+    k = base.as_strided((1, 6, 1, 1, 64), (7, 72, 5, 3, 1))
+    v = base.as_strided((1, 6, 1, 1, 64), (9, 72, 1, 4096, 1))
+    for call in (module.kv4_write, module.kv4_read):
+        with pytest.raises(AssertionError, match="current device"):
+            call(geom, pages, pool, slots, k, v, 0)
+        with pytest.raises(AssertionError, match="one shape and stride"):
+            call(geom, pages, pool, slots, k, base.as_strided((1, 6, 1, 1, 64), (7, 80, 5, 3, 1)), 0)
+        with pytest.raises(AssertionError, match="one behind the other"):
+            call(geom, pages, pool, slots, *[base.as_strided((1, 2, 3, 1, 64), (7, 256, 64, 64, 1))] * 2, 0)
+    q = base.as_strided((1, 3, 1, 1, 64), (3, 64, 5, 9, 1))
+    with pytest.raises(AssertionError, match="current device"):
+        module.kv4_attn(geom, pages, pool, q, q, torch.zeros(1 << 20, dtype=torch.uint8), None, 0.0, 0)
+
+
+def test_one_layer_has_no_distance_to_the_next(lib, monkeypatch):
+    geom, pages, note = cf.make_geom(1, 1, 64, torch.bfloat16, 4096, 1e4), _pages(), Noting()
+    pool = torch.zeros(1 << 20, dtype=torch.uint8).as_strided((1, cf.cf_kv4_layer_bytes(geom, pages)), (3, 1))
+    q = torch.zeros(4096, dtype=torch.bfloat16).as_strided((1, 3, 1, 1, 64), (3, 64, 5, 9, 1))
+    monkeypatch.setattr(M, "_require_here", lambda *t: None)
+    monkeypatch.setattr(binding, "load_library", lambda: note)
+    monkeypatch.setattr(binding, "_stream", lambda s: None)
+    M.kv4_attn(geom, pages, pool, q, q, torch.zeros(1 << 20, dtype=torch.uint8), None, 0.0, None)
+    (_, a), = note.seen
+    assert (a[5], a[7], a[10]) == (0, 0, 0)
+
+
+@pytest.mark.parametrize("module", ["native", "ctypes"])
+@pytest.mark.parametrize("shape", [(2, 0, 3, 2, 64), (2, 3, 0, 2, 64), (1, 0, 2, 64)])
+def test_no_rows_pass_the_checks_of_layout(lib, module, shape):
+    module = binding._load_native(cf_build.NATIVE_PATH) if module == "native" else M
+    geom, pages = cf.make_geom(2, 2, 64, torch.bfloat16, 4096, 1e4), _pages()
+    pool = torch.zeros((shape[0], cf.cf_kv4_layer_bytes(geom, pages)), dtype=torch.uint8)
+    k = torch.zeros(shape, dtype=torch.bfloat16)
+    with pytest.raises(AssertionError, match="current device"):
+        module.kv4_write(geom, pages, pool, torch.zeros(0, dtype=torch.int64), k, k, 0)
