@@ -510,8 +510,8 @@ size_t cf_kv4_attn_workspace_bytes(const cf_geom* geom, const cf_pages* pages, i
  * Keys and values enter the products exactly, queries of bf16 storage too (what lies below 2^-17 of a query's largest
  * component loses last bits, 2^-25 of it); probabilities are rounded to 11 bits (fp32 storage: queries and probabilities to
  * 22), sums are fp32.  (bf16, head_dim 128, more than 56 query heads x tokens per kv head: keys and values whose scales differ
- * by more than 2^28 from the largest among 16 rows lose what lies 2^-38 below that row's.)  A table entry beyond the pool, or
- * more rows than the table has room for, raises CF_ERR_RANGE in the status word; such a request's results mean nothing. */
+ * by more than 2^28 from the largest among 16 rows lose what lies 2^-38 below that row's.)  The table may name a page several
+ * times, for several requests or in one (zeros for a warm-up, a passage that is shared).  A table entry beyond the pool, or more rows than the table has room for, raises CF_ERR_RANGE in the status word; such a request's results mean nothing. */
 int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q,
                 int64_t q_layer_stride, const void* kv4, int64_t kv4_layer_stride, float softmax_scale, void* out,
                 int64_t out_layer_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);

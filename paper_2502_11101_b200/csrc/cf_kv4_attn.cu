@@ -130,6 +130,7 @@ template <int N> __device__ __forceinline__ void lds(uint32_t a, uint32_t (&w)[N
 template <int D>
 struct Feeder {
     static constexpr int kBytes = block_bytes(D);
+    static constexpr int kNone = INT_MIN;         // no distance: a pool of 2^31 blocks has over 2 TB
     const PagesView& pv;
     const Kv4Args& a;
     const Line& line;
@@ -138,7 +139,8 @@ struct Feeder {
     int first, stride, lane;
     int ready, used;                              // steps that the lanes have looked up, one each; how many of them were issued
     const unsigned char* address;                 // a lane's step: its first block,
-    int second;                                   // and how many blocks behind that its second one lies (0: it has none)
+    int second;                                   // and how many blocks behind that its second one lies (in the same one, 0, where a
+                                                  // table names a page of 16 rows twice in a row), kNone where it has none
     uint32_t ring, bars;
     unsigned issued;
     bool ended;
@@ -165,8 +167,8 @@ struct Feeder {
                     const int column = a.blocks_per_page.quotient(block), in_page = block - column * per_page;
                     const int head = a.tiles.quotient(p.unit), page = page_of(p.request, p.rows, column);
                     address = a.kv4 + (size_t)p.layer * a.kv4_layer_stride + (((size_t)page * a.n_kv_heads + head) * per_page + in_page) * kBytes;
-                    second = (block + 1) * kBlockRows >= p.rows ? 0 : 1;
-                    if (second != 0 && in_page + 1 == per_page)
+                    second = (block + 1) * kBlockRows >= p.rows ? kNone : 1;
+                    if (second != kNone && in_page + 1 == per_page)
                         second = (page_of(p.request, p.rows, column + 1) - page) * a.n_kv_heads * per_page - in_page;
                 }
                 step += ready * stride;
@@ -192,9 +194,9 @@ struct Feeder {
         }
         if (lane == used) {
             const uint32_t stage = issued % kStages, bar = bars + 8 * stage, to = ring + stage * kStepBlocks * kBytes;
-            mbar_expect_tx(bar, second != 0 ? 2 * kBytes : kBytes);
+            mbar_expect_tx(bar, second != kNone ? 2 * kBytes : kBytes);
             copy(to, address, second == 1 ? 2 * kBytes : kBytes, bar);
-            if (second != 0 && second != 1) copy(to + kBytes, address + (long long)second * kBytes, kBytes, bar);
+            if (second != kNone && second != 1) copy(to + kBytes, address + (long long)second * kBytes, kBytes, bar);
         }
         ++used;
         ++issued;

@@ -6,7 +6,7 @@ import torch
 import paper_2502_11101_b200 as cf
 from oracle import paged_oracle as P
 from paper_2502_11101_b200 import marshal_ctypes
-from tests.test_gpu_paged import DTYPES, Pages
+from tests.test_gpu_paged import DTYPES, Pages, _attend, _check_attention, _filled
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +41,31 @@ def test_rows_out_of_a_fused_projection(marshal, dtype, dim, layers, requests, t
     for x, got in ((k, kb), (v, vb)):
         assert torch.equal(got.cpu(), torch.from_numpy(P.numbers(*P.quantise(x.double().cpu().numpy()))).to(DTYPES[dtype]))
     assert (back[..., 2 * n:] == 55.0).all()
+
+
+# hq, hkv, q_len, columns of the table: short caches by clusters, shares of the line, few columns and many, the tensor-core kernel
+FORMS = [(4, 4, 1, 0), (4, 4, 1, 3000), (1, 1, 1, 0), (1, 1, 1, 3000), (8, 1, 1, 0), (8, 1, 1, 3000), (28, 4, 1, 0), (28, 4, 1, 3000), (12, 1, 6, 0),
+         (12, 4, 24, 0)]
+
+
+@pytest.mark.parametrize("pattern", ["one", "pairs"])
+@pytest.mark.parametrize("hq,hkv,q_len,cols", FORMS)
+def test_a_table_may_name_a_page_twice_in_a_row(hq, hkv, q_len, cols, pattern):
+    """Pages of 16 rows: a step's second block is its first one.  As a table of zeros has it (a warm-up, a capture), or a passage
+    that is repeated."""
+    dim, columns = 128, 20
+    geom = cf.make_geom(hq, hkv, dim, torch.bfloat16, 32768, 1e6)
+    lengths = [320, 23, 175]
+    pages, pool, kept = _filled(geom, hkv, dim, [96, 90, 80], 16, 1, seed=hq, cols=cols or columns)
+    _attend(geom, pages, pool, torch.randn((1, 3, q_len, hq, dim), device="cuda").bfloat16())     # leaves other rows in shared memory
+    repeated = []
+    for b, n in enumerate(lengths):
+        at = [0 if pattern == "one" else i // 2 % 5 for i in range(columns)]
+        k, v = [np.concatenate([x[16 * i:16 * i + 16] for i in at])[:n] for x in kept[0][b]]
+        pages.table[b, :columns] = pages.table[b, torch.tensor(at, device="cuda")].clone()
+        repeated.append((k, v))
+    pages.rows.copy_(torch.tensor(lengths, dtype=torch.int32))
+    q = torch.randn((1, 3, q_len, hq, dim), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    assert cf.cf_pages_status(pages.desc) == 0
+    _check_attention(geom, out, lse, q, [repeated], dim ** -0.5)
