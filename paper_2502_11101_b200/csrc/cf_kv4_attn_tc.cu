@@ -60,23 +60,25 @@ struct TcShared {
 };
 constexpr int kTcSmem = 1024 + 2 * kTiles * kKeyTile + kRaw * kRawTile + (int)sizeof(TcShared);
 
-// A bounded wait of a whole warp, the same answer in every lane: three instructions a turn, of which there are a hundred for each
-// tile among eighteen warps (with a look at the clock and the abort flag in every turn waiting took two fifths of the issue
-// slots).  The limit is a number of turns, each of which the hardware holds for a hundred cycles or so.
-constexpr uint32_t kWaitTurns = 1u << 23;
+// A bounded wait of a whole warp, the same answer in every lane: what a turn gives may differ from lane to lane, so the lanes vote
+// on it.  There are a hundred turns for each tile among eighteen warps: the clock and the abort flag are looked at once in
+// kWaitTurns of them (in every turn, waiting took two fifths of the issue slots), and turns after the first are not inlined (where
+// they are 47.0 us, see launch_kv4_attn_tc).
+constexpr int kWaitTurns = 256;
+__device__ __noinline__ bool role_wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+    const long long t0 = clock64();
+    while (true) {
+#pragma unroll 1
+        for (int n = 0; n < kWaitTurns; ++n)
+            if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+        if (__any_sync(0xffffffffu, *abort_flag != 0 || clock64() - t0 > kWaitLimitCycles)) {
+            *abort_flag = 1;
+            return false;
+        }
+    }
+}
 __device__ __forceinline__ bool role_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-    uint32_t ok;
-    asm volatile(
-        "{\n.reg .pred p, more;\n.reg .u32 n;\nmov.u32 n, 0;\n"
-        "AGAIN:\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n@p bra.uni DONE;\n"
-        "add.u32 n, n, 1;\nsetp.lt.u32 more, n, %3;\n@more bra.uni AGAIN;\n"
-        "DONE:\nselp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity), "n"(kWaitTurns)
-        : "memory");
-    if (__all_sync(0xffffffffu, ok != 0)) return true;
-    *abort_flag = 1;
-    return false;
+    return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || role_wait_on(bar, parity, abort_flag);
 }
 // fp16 x fp16 -> fp32, A and K-major B; B may be MN-major.
 __device__ __forceinline__ uint32_t instr_desc_f16(int n, bool b_mn_major) {
@@ -618,7 +620,7 @@ bool kv4_attn_tc_supported(const cf_geom* g, int columns, double units) {
     return g->dtype == CF_BF16 && g->head_dim == kD && columns > 56 && units >= 8;
 }
 
-// 24 query tokens over 4 requests of 4-16 K rows, 28/4 heads (168 columns): 46.6 us with the join of the parts, 77 by the kernel of
+// 24 query tokens over 4 requests of 4-16 K rows, 28/4 heads (168 columns): 45.1 us with the join of the parts, 77 by the kernel of
 // cf_kv4_attn.cu; 13.7 GFLOP, 0.18 of the measured peak.  A tile of 64 keys takes 1700 cycles, of which its products are 512: a
 // softmax group is busy for 3400 of every two tiles, the warps of the values for 1650 of each, the MMA warp for 1600, all with
 // latencies (a wait for a barrier that is complete takes 200) at 0.45 of the issue slots.  So no role alone is what bounds it:
