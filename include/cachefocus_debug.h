@@ -47,6 +47,14 @@ int cf_debug_attn_kernel(const cf_geom* geom, const cf_batch* batch, int32_t n_l
  * number of parts that are read from there on, one of every share (none where it is not positive).  Host arithmetic only. */
 int cf_debug_cut_row(uint32_t word, int32_t n_ctas, int32_t ctas_per_share, int32_t* first, int32_t* n_parts);
 
+/* cf_kv4_attn with another limit on its waits (1 .. 2e9 SM clocks; 2e6 is about a millisecond) and, with copies = 0, without the
+ * copies that the first of them waits for, so that waits run out: the call then ends by itself with CF_ERR_TIMEOUT in the pages'
+ * status word, and the device stays usable.  `out` and `lse` mean nothing after that. */
+int cf_debug_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q,
+                      int64_t q_layer_stride, const void* kv4, int64_t kv4_layer_stride, float softmax_scale, void* out,
+                      int64_t out_layer_stride, float* lse, void* workspace, size_t workspace_bytes, int64_t limit_cycles,
+                      int32_t copies, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

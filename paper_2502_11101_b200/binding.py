@@ -37,7 +37,7 @@ EXPORTS = ["cf_error_string", "cf_allocate_positions", "cf_schedule_linear", "cf
            "cf_decode_workspace_bytes", "cf_decode_attn", "cf_decode_append", "cf_pages_init",
            "cf_pages_resize", "cf_pages_status", "cf_kv4_layer_bytes", "cf_kv4_write", "cf_kv4_read", "cf_kv4_attn_workspace_bytes",
            "cf_kv4_attn", "cf_set_attn_path", "cf_profile_begin", "cf_profile_end", "cf_debug_wait_timeout",
-           "cf_debug_attn_kernel", "cf_debug_cut_row"]
+           "cf_debug_attn_kernel", "cf_debug_cut_row", "cf_debug_kv4_attn"]
 _SIZE_T_EXPORTS = ("cf_attn_workspace_bytes", "cf_attn_workspace_bytes_layers", "cf_attn_workspace_bytes_full",
                    "cf_attn_workspace_bytes_slots", "cf_attn_workspace_bytes_slots_full",
                    "cf_run_stack_workspace_bytes", "cf_decode_plan_bytes", "cf_decode_workspace_bytes", "cf_kv4_layer_bytes",
@@ -181,6 +181,7 @@ def load_library() -> ctypes.CDLL:
     lib.cf_kv4_attn_workspace_bytes.restype = ctypes.c_size_t
     lib.cf_kv4_attn_workspace_bytes.argtypes = [gp, pp, i32, i32]
     lib.cf_kv4_attn.argtypes = [gp, pp, i32, i32, vp, i64, vp, i64, ctypes.c_float, vp, i64, vp, vp, ctypes.c_size_t, vp]
+    lib.cf_debug_kv4_attn.argtypes = lib.cf_kv4_attn.argtypes[:-1] + [i64, i32, vp]
     lib.cf_set_attn_path.argtypes = [i32]
     lib.cf_profile_begin.argtypes = [i32]
     lib.cf_profile_end.argtypes = [vp, i32, vp]
@@ -678,6 +679,15 @@ def cf_kv4_attn(geom: cf_geom, pages: cf_pages, kv4: torch.Tensor, q: torch.Tens
     """q, out [n_layers, B, q_len, Hq, D]; kv4 uint8 [n_layers, ...], a layer dense; lse [n_layers, B, Hq, q_len].  Dimension 0 may
     be strided."""
     _check(_native().kv4_attn(geom, pages, kv4, q, out, workspace, lse, softmax_scale, stream), "cf_kv4_attn")
+
+
+def cf_debug_kv4_attn(geom: cf_geom, pages: cf_pages, kv4: torch.Tensor, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
+                      limit_cycles: int, copies: bool = True, lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """cf_kv4_attn on dense tensors whose waits run out after `limit_cycles`, for certain without its copies."""
+    assert q.is_contiguous() and out.is_contiguous() and kv4.is_contiguous()
+    _check(load_library().cf_debug_kv4_attn(ctypes.byref(geom), ctypes.byref(pages), q.shape[0], q.shape[2], q.data_ptr(), q.stride(0),
+                                            kv4.data_ptr(), kv4.stride(0), 0.0, out.data_ptr(), out.stride(0), _ptr(lse), workspace.data_ptr(),
+                                            workspace.numel(), limit_cycles, int(copies), _stream(stream)), "cf_debug_kv4_attn")
 
 
 def plan_field(plan: torch.Tensor, layout: cf_plan_layout, name: str, count: int, dtype=torch.int32) -> torch.Tensor:

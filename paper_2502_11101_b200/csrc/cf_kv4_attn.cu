@@ -157,7 +157,7 @@ struct Feeder {
         int step = *next;
         __syncwarp();
         ready = used = 0;
-        while (p.left > 0) {
+        while (p.left > 0 && !a.no_copies) {
             const int last = p.last_step(line.cost);
             const int n = step < last ? (last - step + stride - 1) / stride : 0;
             if (n > 0) {
@@ -370,7 +370,7 @@ kv4_attn_kernel(Kv4Args args, PagesView pv) {
 
         for (int step = start + first_step; step < last; step += stride) {
             const uint32_t stage = taken % kStages, blocks = ring + stage * kStepBlocks * kBytes;
-            const bool came = given_up || tc::mbar_wait(bars + 8 * stage, taken / kStages & 1, &s_abort);
+            const bool came = given_up || tc::mbar_wait(bars + 8 * stage, taken / kStages & 1, &s_abort, a.wait_limit);
             ++taken;
             // S^T of 32 keys: s[block][half][own column]
             float s[kStepBlocks][2][kOwn];
@@ -867,24 +867,9 @@ int launch_attn_typed(const Kv4Args& a, const PagesView& pv, const Cut& c, int h
     return head_dim == 128 ? launch_attn_cut<T, 128>(a, pv, c, stream) : launch_attn_cut<T, 64>(a, pv, c, stream);
 }
 
-}  // namespace
-
-}  // namespace cf
-
-using namespace cf;
-
-extern "C" {
-
-size_t cf_kv4_attn_workspace_bytes(const cf_geom* geom, const cf_pages* pages, int32_t q_len, int32_t n_layers) {
-    if (check_attn(geom, pages, q_len, n_layers) != CF_OK) return 0;
-    const Cut c = cut_of(geom, pages, q_len, n_layers);
-    const size_t rows = 2 * (size_t)c.n_shares * c.tile;
-    return round_up(rows * geom->head_dim * 4) + round_up(rows * 8) + round_up((size_t)c.marks * sizeof(int4));
-}
-
-int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q,
-                int64_t q_layer_stride, const void* kv4, int64_t kv4_layer_stride, float softmax_scale, void* out,
-                int64_t out_layer_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+int run_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q, int64_t q_layer_stride, const void* kv4,
+             int64_t kv4_layer_stride, float softmax_scale, void* out, int64_t out_layer_stride, float* lse, void* workspace, size_t workspace_bytes,
+             int wait_limit, bool copies, void* stream) {
     const int rc = check_attn(geom, pages, q_len, n_layers);
     if (rc != CF_OK) return rc;
     if (!q || !kv4 || !out || !workspace) return CF_ERR_INVALID_ARG;
@@ -920,6 +905,7 @@ int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, in
         a.cluster = Divisor(c.cluster), a.units_of = Divisor(geom->n_kv_heads * c.tiles), a.requests = Divisor(pages->n_requests);
     }
     a.scale_log2 = scale * kLog2e;
+    a.no_copies = !copies, a.wait_limit = wait_limit;
     const PagesView pv = make_pages_view(pages);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (c.tc) {
@@ -928,6 +914,37 @@ int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, in
     }
     return geom->dtype == CF_BF16 ? launch_attn_typed<__nv_bfloat16>(a, pv, c, geom->head_dim, s)
                                   : launch_attn_typed<float>(a, pv, c, geom->head_dim, s);
+}
+
+}  // namespace
+
+}  // namespace cf
+
+using namespace cf;
+
+extern "C" {
+
+size_t cf_kv4_attn_workspace_bytes(const cf_geom* geom, const cf_pages* pages, int32_t q_len, int32_t n_layers) {
+    if (check_attn(geom, pages, q_len, n_layers) != CF_OK) return 0;
+    const Cut c = cut_of(geom, pages, q_len, n_layers);
+    const size_t rows = 2 * (size_t)c.n_shares * c.tile;
+    return round_up(rows * geom->head_dim * 4) + round_up(rows * 8) + round_up((size_t)c.marks * sizeof(int4));
+}
+
+int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q,
+                int64_t q_layer_stride, const void* kv4, int64_t kv4_layer_stride, float softmax_scale, void* out,
+                int64_t out_layer_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    return run_attn(geom, pages, n_layers, q_len, q, q_layer_stride, kv4, kv4_layer_stride, softmax_scale, out, out_layer_stride, lse, workspace,
+                    workspace_bytes, (int)tc::kWaitLimitCycles, true, stream);
+}
+
+int cf_debug_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q,
+                      int64_t q_layer_stride, const void* kv4, int64_t kv4_layer_stride, float softmax_scale, void* out,
+                      int64_t out_layer_stride, float* lse, void* workspace, size_t workspace_bytes, int64_t limit_cycles,
+                      int32_t copies, void* stream) {
+    if (limit_cycles <= 0 || limit_cycles > tc::kWaitLimitCycles) return CF_ERR_INVALID_ARG;
+    return run_attn(geom, pages, n_layers, q_len, q, q_layer_stride, kv4, kv4_layer_stride, softmax_scale, out, out_layer_stride, lse, workspace,
+                    workspace_bytes, (int)limit_cycles, copies != 0, stream);
 }
 
 }  // extern "C"

@@ -25,6 +25,8 @@ struct Kv4Args {
     Divisor cluster, units_of, requests;          // of short caches: CTAs of a unit (0: shares of the line); units of a (layer, request)
     long long least_share;
     float scale_log2;
+    int no_copies;                                // nothing is copied, so that every wait runs out (cf_debug_kv4_attn)
+    int wait_limit;                               // of a wait, in cycles
 };
 
 // What a call runs once costs more than its cycles: its instructions come from memory.  So no divisions of 64 bits where 32 do, and

@@ -51,6 +51,7 @@ struct TcShared {
     unsigned long long based[4], exchanged[4];    // by 32 query columns: the base of a tile is known; what the groups tell each other at the end
     unsigned tmem_base;
     volatile int abort_flag;
+    int wait_limit;
     float key_unit[kUnits][kBlocks];              // 2^c of a tile's blocks
     int value_unit[kUnits][kBlocks];              // c
     int o_unit[2][4];                             // of O, by the last tiles of the two groups and, as `based`, by 32 query columns
@@ -65,20 +66,20 @@ constexpr int kTcSmem = 1024 + 2 * kTiles * kKeyTile + kRaw * kRawTile + (int)si
 // kWaitTurns of them (in every turn, waiting took two fifths of the issue slots), and turns after the first are not inlined (where
 // they are 47.0 us, see launch_kv4_attn_tc).
 constexpr int kWaitTurns = 256;
-__device__ __noinline__ bool role_wait_on(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+__device__ __noinline__ bool role_wait_on(uint32_t bar, uint32_t parity, TcShared* sh) {
     const long long t0 = clock64();
     while (true) {
 #pragma unroll 1
         for (int n = 0; n < kWaitTurns; ++n)
             if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-        if (__any_sync(0xffffffffu, *abort_flag != 0 || clock64() - t0 > kWaitLimitCycles)) {
-            *abort_flag = 1;
+        if (__any_sync(0xffffffffu, sh->abort_flag != 0 || clock64() - t0 > sh->wait_limit)) {
+            sh->abort_flag = 1;
             return false;
         }
     }
 }
-__device__ __forceinline__ bool role_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-    return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || role_wait_on(bar, parity, abort_flag);
+__device__ __forceinline__ bool role_wait(uint32_t bar, uint32_t parity, TcShared* sh) {
+    return __all_sync(0xffffffffu, mbar_try_wait(bar, parity)) || role_wait_on(bar, parity, sh);
 }
 // fp16 x fp16 -> fp32, A and K-major B; B may be MN-major.
 __device__ __forceinline__ uint32_t instr_desc_f16(int n, bool b_mn_major) {
@@ -229,7 +230,6 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
     unsigned char* smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
     unsigned char *s_k = smem, *s_v = smem + kTiles * kKeyTile, *s_raw = smem + 2 * kTiles * kKeyTile;
     TcShared* sh = reinterpret_cast<TcShared*>(s_raw + kRaw * kRawTile);
-    volatile int* abort_flag = &sh->abort_flag;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     asm volatile("fence.proxy.async;" ::: "memory");         // what earlier kernels wrote is read by bulk copies
 
@@ -265,7 +265,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 mbar_init(smem_u32(&sh->exchanged[i]), 2);
             }
             mbar_init(smem_u32(&sh->q_full), 8);
-            sh->abort_flag = 0;
+            sh->abort_flag = 0, sh->wait_limit = a.wait_limit;
             for (int i = 0; i < kUnits; ++i) sh->nan_unit[i] = 0;
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
@@ -303,8 +303,8 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 }
                 for (int i = 0; ok && i < min(8, last - t0); ++i, ++g) {
                     const int stage = g % kRaw;
-                    if (g >= kRaw) ok = role_wait(smem_u32(&sh->raw_free[stage]), (g / kRaw - 1) & 1, abort_flag);
-                    if (ok && (lane >> 2) == i) {
+                    if (g >= kRaw) ok = role_wait(smem_u32(&sh->raw_free[stage]), (g / kRaw - 1) & 1, sh);
+                    if (ok && (lane >> 2) == i && !a.no_copies) {
                         const uint32_t bar = smem_u32(&sh->raw_full[stage]);
                         if (from) {
                             mbar_expect_tx(bar, kBlockBytes);
@@ -323,7 +323,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
         const uint32_t idesc_s = instr_desc_f16(kKeys, false), idesc_o = instr_desc_f16(kD, true);
         auto issue_pv = [&](int tile, bool first) {          // O (+)= P V of a tile
             const int b = tile & 1, v = tile % kTiles;
-            ok = role_wait(smem_u32(&sh->p_ready[b]), (tile >> 1) & 1, abort_flag);
+            ok = role_wait(smem_u32(&sh->p_ready[b]), (tile >> 1) & 1, sh);
             if (!ok) return;
             tc_fence_after();
             if (elect_one()) {
@@ -338,12 +338,12 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
         for (; ok && p.left > 0; line.next_unit(p)) {
             const int start = p.first_step(cost), last = p.last_step(cost);
             if (last <= start) continue;
-            ok = role_wait(smem_u32(&sh->q_full), ordinal & 1, abort_flag);
+            ok = role_wait(smem_u32(&sh->q_full), ordinal & 1, sh);
             for (int t = start; ok && t < last + kAhead; ++t) {
                 if (t < last) {
                     const int k = g % kTiles;
                     // the values too: with S the softmax has the units of both
-                    ok = role_wait(smem_u32(&sh->full[k]), (g / kTiles) & 1, abort_flag);
+                    ok = role_wait(smem_u32(&sh->full[k]), (g / kTiles) & 1, sh);
                     if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {                       // over S of the tile four before, whose P has been waited for
@@ -372,9 +372,9 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
             const int all_see = p.rows - a.q_len + 1 + a.group.quotient((p.unit - head * (int)a.tiles.d) * kTcColumns);
             for (int t = start; ok && t < last; ++t, ++g) {
                 const int k = g % kTiles, stage = g % kRaw, row0 = t * kKeys + block * kBlockRows;
-                ok = role_wait(smem_u32(&sh->raw_full[stage]), (g / kRaw) & 1, abort_flag);
+                ok = role_wait(smem_u32(&sh->raw_full[stage]), (g / kRaw) & 1, sh);
                 // the tile that was in this buffer has been read
-                if (ok && g >= kTiles) ok = role_wait(smem_u32(values ? &sh->v_free[k] : &sh->k_free[k]), (g / kTiles - 1) & 1, abort_flag);
+                if (ok && g >= kTiles) ok = role_wait(smem_u32(values ? &sh->v_free[k] : &sh->k_free[k]), (g / kTiles - 1) & 1, sh);
                 if (!ok) break;
                 const unsigned char* raw = s_raw + stage * kRawTile + block * kBlockBytes;
                 bool nan;
@@ -409,7 +409,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
             sh->row[turn][group][r] = mine;
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->exchanged[quad]));
-            ok = role_wait(smem_u32(&sh->exchanged[quad]), turn, abort_flag);
+            ok = role_wait(smem_u32(&sh->exchanged[quad]), turn, sh);
             return sh->row[turn][group ^ 1][r];
         };
         for (; ok && p.left > 0; line.next_unit(p)) {
@@ -462,7 +462,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 const int* value_unit = sh->value_unit[g % kUnits];
                 const float* key_unit = sh->key_unit[g % kUnits];
                 const uint32_t s_addr = lane_tmem + kTmemS + (g & 3) * kKeys;
-                ok = role_wait(smem_u32(&sh->s_full[g & 3]), (g >> 2) & 1, abort_flag);
+                ok = role_wait(smem_u32(&sh->s_full[g & 3]), (g >> 2) & 1, sh);
                 if (!ok) break;
                 tc_fence_after();
                 const bool masked = (t + 1) * kKeys > all_see;
@@ -475,7 +475,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 float from = -INFINITY;
                 o_unit = -1000;
                 if (t > start) {
-                    ok = role_wait(smem_u32(&sh->based[quad]), (g - 1) & 1, abort_flag);
+                    ok = role_wait(smem_u32(&sh->based[quad]), (g - 1) & 1, sh);
                     if (!ok) break;
                     from = sh->base[group ^ 1][r];
                     o_unit = sh->o_unit[group ^ 1][quad];
@@ -492,7 +492,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 if (t > start && __any_sync(0xffffffffu, from != now || o_unit != now_unit)) {
                     // O in tensor memory, when the tile before is in it
                     const float f = (from == now || from == -INFINITY ? 1.f : fast_exp2(from - now)) * exp2f((float)(o_unit - now_unit));
-                    ok = role_wait(smem_u32(&sh->o_done[group ^ 1]), ((g - 1) >> 1) & 1, abort_flag);
+                    ok = role_wait(smem_u32(&sh->o_done[group ^ 1]), ((g - 1) >> 1) & 1, sh);
                     if (!ok) break;
                     tc_fence_after();
 #pragma unroll 1
@@ -507,7 +507,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 }
                 o_unit = now_unit;
                 if (g >= 2) {                                // PV has read the P that the group left last
-                    ok = role_wait(smem_u32(&sh->o_done[group]), ((g >> 1) - 1) & 1, abort_flag);
+                    ok = role_wait(smem_u32(&sh->o_done[group]), ((g >> 1) - 1) & 1, sh);
                     if (!ok) break;
                     tc_fence_after();
                 }
@@ -533,7 +533,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
                 o_unit = sh->o_unit[(g - 1) & 1][quad];
             }
             // results, or a part of them
-            ok = role_wait(smem_u32(&sh->o_done[(g - 1) & 1]), ((g - 1) >> 1) & 1, abort_flag);
+            ok = role_wait(smem_u32(&sh->o_done[(g - 1) & 1]), ((g - 1) >> 1) & 1, sh);
             if (!ok) break;
             tc_fence_after();
             unsigned bad = 0;                                // groups of dims that a NaN reached
@@ -596,7 +596,14 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
     tc_fence_before();
     __syncthreads();
     if (sh->abort_flag) {
-        // a wait expired: the copies in flight get the time to land before the shared memory is given back
+        // A wait expired.  What the share's units leave for the join is not all there, and a mark that was not written would send it
+        // anywhere: nothing is joined of the units that begin here.
+        if (warp == 0) {
+            for (Walk w = line.find(begin, mine, per_layer); w.left > 0; line.next_unit(w))
+                if (lane == 0 && w.at <= cost && w.end() > cost)
+                    a.marks[a.marks_by_unit ? (w.layer * pv.n_requests + w.request) * line.units + w.unit : share] = make_int4(0, 0, 0, 0);
+        }
+        // the copies in flight get the time to land before the shared memory is given back
         if (tid == 0) {
             const long long t0 = clock64();
             while (clock64() - t0 < kWaitLimitCycles / 64) {}

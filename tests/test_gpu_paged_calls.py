@@ -69,3 +69,58 @@ def test_a_table_may_name_a_page_twice_in_a_row(hq, hkv, q_len, cols, pattern):
     out, lse = _attend(geom, pages, pool, q)
     assert cf.cf_pages_status(pages.desc) == 0
     _check_attention(geom, out, lse, q, [repeated], dim ** -0.5)
+
+
+def _marks(work, units):
+    """What the attention kernel leaves for the join: a mark of four numbers for each unit, or for each share (an SM's) where those are
+    fewer, at the end of the workspace."""
+    n = min(units, torch.cuda.get_device_properties(0).multi_processor_count)
+    return work[work.numel() - -(-16 * n // 256) * 256:][:16 * n].view(torch.int32).view(n, 4)
+
+
+@pytest.mark.parametrize("hq,hkv,q_len,requests", [(28, 4, 24, 3), (12, 1, 20, 9), (32, 8, 20, 30)])
+def test_waits_of_the_tensor_core_kernel_that_run_out(hq, hkv, q_len, requests):
+    """The call ends with an error that the host reads, and without marks that were not written: the join would take anything for
+    one, and read and write where it says.  (Here the workspace is all -1, which the join passes over.)"""
+    geom = cf.make_geom(hq, hkv, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, hkv, 128, [700 + 31 * i % 400 for i in range(requests)], 16, 1, seed=hq)
+    q = torch.randn((1, requests, q_len, hq, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    right, right_lse = _attend(geom, pages, pool, q)
+    units = requests * hkv * -(-hq // hkv * q_len // 128)
+    work = torch.empty(cf.cf_kv4_attn_workspace_bytes(geom, pages.desc, q_len, 1), dtype=torch.uint8, device="cuda")
+    for limit, copies in ((2000000, False), (1, False), (1, True), (20000, True), (2000000, True)):
+        work.fill_(255)
+        out, lse = torch.full_like(q, 99.0), torch.full_like(right_lse, 99.0)
+        pages.status.zero_()
+        cf.cf_debug_kv4_attn(geom, pages.desc, pool, q, out, work, limit, copies, lse=lse)
+        status, marks = cf.cf_pages_status(pages.desc), _marks(work, units)
+        if not copies:
+            assert status == cf.CF_ERR_TIMEOUT and (marks == 0).all() and (out == 99.0).all() and (lse == 99.0).all()
+        elif status == 0:
+            assert torch.equal(out, right) and torch.equal(lse, right_lse)
+        else:
+            assert status == cf.CF_ERR_TIMEOUT
+        assert (marks >= 0).all()
+    pages.status.zero_()
+    out, lse = _attend(geom, pages, pool, q)
+    assert cf.cf_pages_status(pages.desc) == 0 and torch.equal(out, right) and torch.equal(lse, right_lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,q_len,cols", [(4, 4, 1, 0), (4, 4, 1, 3000), (28, 4, 1, 0), (28, 4, 1, 3000), (12, 1, 2, 0), (12, 1, 2, 3000)])
+def test_waits_that_run_out(dtype, hq, hkv, q_len, cols):
+    geom = cf.make_geom(hq, hkv, 128, DTYPES[dtype], 32768, 1e6)
+    pages, pool, kept = _filled(geom, hkv, 128, [700, 40, 333], 32, 1, seed=hq, cols=cols or None)
+    q = torch.randn((1, 3, q_len, hq, 128), generator=torch.Generator().manual_seed(4)).to(DTYPES[dtype]).cuda()
+    right, right_lse = _attend(geom, pages, pool, q)
+    work = torch.full((cf.cf_kv4_attn_workspace_bytes(geom, pages.desc, q_len, 1),), 255, dtype=torch.uint8, device="cuda")
+    for limit, copies in ((2000000, False), (1, False), (1, True), (2000000, True)):
+        out, lse = torch.full_like(q, 99.0), torch.full_like(right_lse, 99.0)
+        pages.status.zero_()
+        cf.cf_debug_kv4_attn(geom, pages.desc, pool, q, out, work, limit, copies, lse=lse)
+        status = cf.cf_pages_status(pages.desc)
+        assert status == cf.CF_ERR_TIMEOUT if not copies else status in (0, cf.CF_ERR_TIMEOUT)
+        assert status != 0 or torch.equal(out, right) and torch.equal(lse, right_lse)
+    pages.status.zero_()
+    out, lse = _attend(geom, pages, pool, q)
+    assert cf.cf_pages_status(pages.desc) == 0 and torch.equal(out, right) and torch.equal(lse, right_lse)

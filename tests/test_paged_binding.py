@@ -1,6 +1,6 @@
-"""Which rows the calls on the 4-bit pool take: layouts that torch gives to keys and values of one token, one layer, one head.  No
-GPU: tensors of the host pass the checks of layout and are refused for their device, or reach a library that only notes what it
-is given."""
+"""What the calls on the 4-bit pages take and refuse before a GPU is asked: layouts that torch gives to keys and values of one token,
+one layer, one head; limits.  Tensors of the host pass the checks of layout and are refused for their device, or reach a library
+that only notes what it is given."""
 import ctypes
 
 import pytest
@@ -117,3 +117,15 @@ def test_no_rows_pass_the_checks_of_layout(lib, module, shape):
     k = torch.zeros(shape, dtype=torch.bfloat16)
     with pytest.raises(AssertionError, match="current device"):
         module.kv4_write(geom, pages, pool, torch.zeros(0, dtype=torch.int64), k, k, 0)
+
+
+def test_limits_of_waits_that_make_no_sense_are_refused(lib):
+    pages, geom, ref = _pages(), cf.make_geom(4, 2, 64, cf.CF_BF16, 4096, 1e4), ctypes.byref
+    layer = cf.cf_kv4_layer_bytes(geom, pages)
+
+    def call(limit, ws_bytes):
+        return lib.cf_debug_kv4_attn(ref(geom), ref(pages), 1, 1, FAKE, 0, FAKE, layer, 0.0, FAKE, 0, None, FAKE, ws_bytes, limit, 1, None)
+
+    for limit in (0, -1, 2000000001):
+        assert call(limit, 1 << 40) == cf.CF_ERR_INVALID_ARG
+    assert call(1000, 0) == cf.CF_ERR_WORKSPACE
