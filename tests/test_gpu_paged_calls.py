@@ -6,7 +6,7 @@ import torch
 import paper_2502_11101_b200 as cf
 from oracle import paged_oracle as P
 from paper_2502_11101_b200 import marshal_ctypes
-from tests.test_gpu_paged import DTYPES, Pages, _attend, _check_attention, _filled
+from tests.test_gpu_paged import DTYPES, Pages, _attend, _check_attention, _filled, _same_pages
 
 pytestmark = pytest.mark.gpu
 
@@ -124,3 +124,64 @@ def test_waits_that_run_out(dtype, hq, hkv, q_len, cols):
     pages.status.zero_()
     out, lse = _attend(geom, pages, pool, q)
     assert cf.cf_pages_status(pages.desc) == 0 and torch.equal(out, right) and torch.equal(lse, right_lse)
+
+
+@pytest.mark.parametrize("dtype,dim,heads,page_rows,n_rows,layers,pad", [
+    ("bf16", 64, 9, 48, 140001, 1, 0), ("bf16", 128, 7, 16, 100003, 1, 8), ("f32", 128, 5, 64, 63001, 3, 0), ("f32", 64, 13, 32, 90002, 2, 16)])
+def test_many_rows_of_several_heads(dtype, dim, heads, page_rows, n_rows, layers, pad):
+    """Calls of so many rows that a warp takes several heads of its own, the last of them fewer: as the same rows a few at a time, in
+    and out, and as the format says."""
+    gen = torch.Generator(device="cuda").manual_seed(n_rows)
+    n_pages = n_rows // page_rows + 3
+    slots = torch.randperm(n_pages * page_rows, generator=gen, device="cuda")[:n_rows]
+    at = torch.randperm(n_rows, generator=gen, device="cuda")
+    slots[at[:500]], slots[at[500:510]] = -1, n_pages * page_rows + 3
+    slots[-3:] = slots[-3:].abs() % (n_pages * page_rows)
+    geom = cf.make_geom(heads, heads, dim, DTYPES[dtype], 4096, 1e4)
+    pages = Pages(2, page_rows, n_pages, 4)
+    k, v = [(torch.randn((layers, n_rows, heads * dim + pad), generator=gen, device="cuda") * 3).to(DTYPES[dtype])[..., :heads * dim].unflatten(-1, (heads, dim))
+            for _ in range(2)]
+    k[0, 5, 1, 7], v[-1, -1, -1, 33] = float("inf"), float("nan")
+    start = torch.randint(0, 256, (layers, cf.cf_kv4_layer_bytes(geom, pages.desc)), dtype=torch.uint8, generator=gen, device="cuda")
+    pools, backs = [start.clone(), start.clone()], [[torch.full((layers, n_rows, heads, dim), 55.0, dtype=DTYPES[dtype], device="cuda") for _ in range(2)] for _ in range(2)]
+    for pool, back, step in zip(pools, backs, (n_rows, 5000)):
+        for i in range(0, n_rows, step):
+            rows = slice(i, i + step)
+            cf.cf_kv4_write(geom, pages.desc, pool, slots[rows], k[:, rows], v[:, rows])
+            assert cf.cf_pages_status(pages.desc) in (0, cf.CF_ERR_RANGE)
+        for i in range(0, n_rows, step):
+            rows = slice(i, i + step)
+            cf.cf_kv4_read(geom, pages.desc, pool, slots[rows], back[0][:, rows], back[1][:, rows])
+    assert cf.cf_pages_status(pages.desc) == cf.CF_ERR_RANGE
+    assert torch.equal(pools[0], pools[1]) and not torch.equal(pools[0], start)
+    sample = torch.cat([at[500:900], torch.arange(n_rows - 3, n_rows, device="cuda"), torch.arange(8, device="cuda")])
+    kept = (slots[sample] >= 0) & (slots[sample] < n_pages * page_rows)
+    for x, one, few in zip((k, v), *backs):
+        assert torch.equal(one.nan_to_num(nan=1e30), few.nan_to_num(nan=1e30))
+        assert (one[:, slots < 0] == 55.0).all() and (one[:, slots >= n_pages * page_rows] == 55.0).all()
+        want = torch.from_numpy(P.numbers(*P.quantise(x[:, sample].double().cpu().numpy()))).to(DTYPES[dtype])
+        want[:, ~kept.cpu()] = 55.0
+        assert torch.equal(one[:, sample].cpu().nan_to_num(nan=1e30), want.nan_to_num(nan=1e30))
+
+
+@pytest.mark.parametrize("n_requests,page_rows,cols", [(8, 16, 9), (1000, 32, 5), (1024, 16, 6), (2500, 16, 5)])
+@pytest.mark.parametrize("max_new", [None, 1, 70])
+def test_the_lengths_may_be_the_pages_own_for_any_number_of_requests(n_requests, page_rows, cols, max_new):
+    """Eight blocks read the lengths that one of them overwrites, in one round and in several."""
+    rng = np.random.default_rng(n_requests)
+    n_pages = n_requests * cols * 2 // 3
+    got, want = Pages(n_requests, page_rows, n_pages, cols), P.Pool(n_requests, page_rows, n_pages, cols)
+    rows = [int(r) for r in rng.integers(0, cols * page_rows // 2, n_requests)]
+    got.resize(rows)
+    want.resize(rows, 0, None)
+    for extra in (1, page_rows + 1, -7, 0, 1, -page_rows, 3):
+        extra = min(extra, 1) if max_new == 1 else extra
+        slots = None if max_new is None else torch.full((n_requests, max_new), 777, dtype=torch.int64, device="cuda")
+        expect = want.resize(list(want.rows), extra, max_new)
+        cf.cf_pages_resize(got.desc, got.rows, extra, slots)
+        torch.cuda.synchronize()
+        _same_pages(got, want)
+        assert max_new is None or np.array_equal(slots.cpu().numpy(), np.array(expect))
+        assert cf.cf_pages_status(got.desc) in (want.status or {0})
+        want.status.clear()
+        got.status.zero_()
