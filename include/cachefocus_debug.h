@@ -47,6 +47,10 @@ int cf_debug_attn_kernel(const cf_geom* geom, const cf_batch* batch, int32_t n_l
  * number of parts that are read from there on, one of every share (none where it is not positive).  Host arithmetic only. */
 int cf_debug_cut_row(uint32_t word, int32_t n_ctas, int32_t ctas_per_share, int32_t* first, int32_t* n_parts);
 
+/* How a call of cf_kv4_attn is done: 0 = mma.sync, a share of the work to a warp, 1 = a share to the warps of a CTA, 2 = a cluster of
+ * CTAs to a unit, 3 = tcgen05.  (Without a GPU: for 148 multiprocessors.) */
+int cf_debug_kv4_attn_kernel(const cf_geom* geom, const cf_pages* pages, int32_t q_len, int32_t n_layers, int32_t* which);
+
 /* cf_kv4_attn with another limit on its waits (1 .. 2e9 SM clocks; 2e6 is about a millisecond) and, with copies = 0, without the
  * copies that the first of them waits for, so that waits run out: the call then ends by itself with CF_ERR_TIMEOUT in the pages'
  * status word, and the device stays usable.  `out` and `lse` mean nothing after that. */

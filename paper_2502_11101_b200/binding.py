@@ -37,7 +37,8 @@ EXPORTS = ["cf_error_string", "cf_allocate_positions", "cf_schedule_linear", "cf
            "cf_decode_workspace_bytes", "cf_decode_attn", "cf_decode_append", "cf_pages_init",
            "cf_pages_resize", "cf_pages_status", "cf_kv4_layer_bytes", "cf_kv4_write", "cf_kv4_read", "cf_kv4_attn_workspace_bytes",
            "cf_kv4_attn", "cf_set_attn_path", "cf_profile_begin", "cf_profile_end", "cf_debug_wait_timeout",
-           "cf_debug_attn_kernel", "cf_debug_cut_row", "cf_debug_kv4_attn"]
+           "cf_debug_attn_kernel", "cf_debug_cut_row", "cf_debug_kv4_attn",
+           "cf_debug_kv4_attn_kernel"]
 _SIZE_T_EXPORTS = ("cf_attn_workspace_bytes", "cf_attn_workspace_bytes_layers", "cf_attn_workspace_bytes_full",
                    "cf_attn_workspace_bytes_slots", "cf_attn_workspace_bytes_slots_full",
                    "cf_run_stack_workspace_bytes", "cf_decode_plan_bytes", "cf_decode_workspace_bytes", "cf_kv4_layer_bytes",
@@ -181,6 +182,7 @@ def load_library() -> ctypes.CDLL:
     lib.cf_kv4_attn_workspace_bytes.restype = ctypes.c_size_t
     lib.cf_kv4_attn_workspace_bytes.argtypes = [gp, pp, i32, i32]
     lib.cf_kv4_attn.argtypes = [gp, pp, i32, i32, vp, i64, vp, i64, ctypes.c_float, vp, i64, vp, vp, ctypes.c_size_t, vp]
+    lib.cf_debug_kv4_attn_kernel.argtypes = [gp, pp, i32, i32, vp]
     lib.cf_debug_kv4_attn.argtypes = lib.cf_kv4_attn.argtypes[:-1] + [i64, i32, vp]
     lib.cf_set_attn_path.argtypes = [i32]
     lib.cf_profile_begin.argtypes = [i32]
@@ -679,6 +681,14 @@ def cf_kv4_attn(geom: cf_geom, pages: cf_pages, kv4: torch.Tensor, q: torch.Tens
     """q, out [n_layers, B, q_len, Hq, D]; kv4 uint8 [n_layers, ...], a layer dense; lse [n_layers, B, Hq, q_len].  Dimension 0 may
     be strided."""
     _check(_native().kv4_attn(geom, pages, kv4, q, out, workspace, lse, softmax_scale, stream), "cf_kv4_attn")
+
+
+def cf_debug_kv4_attn_kernel(geom: cf_geom, pages: cf_pages, q_len: int, n_layers: int) -> int:
+    """How a call of cf_kv4_attn is done: 0, 1 shares of warps and of CTAs (mma.sync), 2 clusters (mma.sync), 3 tcgen05."""
+    which = ctypes.c_int32(0)
+    _check(load_library().cf_debug_kv4_attn_kernel(ctypes.byref(geom), ctypes.byref(pages), q_len, n_layers, ctypes.byref(which)),
+           "cf_debug_kv4_attn_kernel")
+    return which.value
 
 
 def cf_debug_kv4_attn(geom: cf_geom, pages: cf_pages, kv4: torch.Tensor, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,

@@ -60,7 +60,7 @@ constexpr int kMostCost = 32;                     // of a unit, in steps
 constexpr int kLeastAlone = 4, kLeastTogether = 8;
 constexpr int kCostAlone = 3, kCostTogether = 16;
 constexpr int kMostCluster = 8;
-constexpr int kClusterSteps = 6, kClusterStepsFew = 9;     // most steps of a warp where a cluster has a unit; with few columns
+constexpr int kClusterSteps = 6, kClusterStepsFew = 9;     // a warp has fewer steps than this where a cluster has a unit; with few columns
 constexpr int kLeastTc = 8, kCostTc = 6;          // of the tensor-core kernel, in steps of its own
 
 // Warps of a CTA, and CTAs of an SM.  With few columns the loop fits 128 registers: 16 warps per SM; without, and with twice the
@@ -799,7 +799,10 @@ Cut cut_of(const cf_geom* g, const cf_pages* p, int q_len, int n_layers) {
         // the room): 12/2 heads, one request of 500, 1000, 2000, 4000, 8000 rows 8.2 / 6.2, 8.5 / 6.2, 8.7 / 7.1, 8.7 / 8.5, 9.0 / 11.5
         // (eight steps a warp); 28/4, eight requests of up to that 10.1 / 7.8, 10.7 / 8.0, 11.6 / 9.2, 12.1 / 11.6, 15.1 / 16.2 (eight);
         // a column a head, 32/32, one of 2000, 4000, 8000 10.6 / 7.9, 11.8 / 9.8, 15.0 / 12.9, two of 4000, 8000 13.3 / 12.0, 19.3 / 19.7
-        // (eight steps), four of 4000 20.1 / 19.7 (eight), eight of 1000, 2000, 4000 15.3 / 11.0, 21.4 / 18.9 (nine), 30.0 / 30.4 (sixteen).
+        // (eight steps), four of 4000 20.1 / 19.7 (eight), eight of 1000, 2000, 4000 15.3 / 11.0, 21.4 / 18.9 (nine), 30.0 / 30.4 (sixteen);
+        // with the whole of six steps, 12/2, one of 6144 8.3 / 9.7, 28/4, eight of them 13.3 / 13.8, of nine with few columns, 2/2, one of
+        // 18432 10.4 / 13.8.  It is the room that counts, not the rows: with room for 32768, 12/2, one of 1011 8.3 instead of 5.9,
+        // 28/4, eight of 1000 10.5 instead of 7.7, 32/32, one of 2000 10.6 instead of 7.8.
         const double steps = ((double)p->table_cols * p->page_rows + kStepRows - 1) / kStepRows;
         int cluster = 1;
         while (cluster < kMostCluster && cluster * c.warps < steps && 2 * units * cluster <= c.ctas) cluster *= 2;
@@ -945,6 +948,15 @@ int cf_debug_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_laye
     if (limit_cycles <= 0 || limit_cycles > tc::kWaitLimitCycles) return CF_ERR_INVALID_ARG;
     return run_attn(geom, pages, n_layers, q_len, q, q_layer_stride, kv4, kv4_layer_stride, softmax_scale, out, out_layer_stride, lse, workspace,
                     workspace_bytes, (int)limit_cycles, copies != 0, stream);
+}
+
+int cf_debug_kv4_attn_kernel(const cf_geom* geom, const cf_pages* pages, int32_t q_len, int32_t n_layers, int32_t* which) {
+    const int rc = check_attn(geom, pages, q_len, n_layers);
+    if (rc != CF_OK) return rc;
+    if (!which) return CF_ERR_INVALID_ARG;
+    const Cut c = cut_of(geom, pages, q_len, n_layers);
+    *which = c.tc ? 3 : c.cluster > 0 ? 2 : c.warps_per_share == 1 ? 0 : 1;
+    return CF_OK;
 }
 
 }  // extern "C"

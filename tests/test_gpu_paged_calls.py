@@ -185,3 +185,32 @@ def test_the_lengths_may_be_the_pages_own_for_any_number_of_requests(n_requests,
         assert cf.cf_pages_status(got.desc) in (want.status or {0})
         want.status.clear()
         got.status.zero_()
+
+
+@pytest.mark.parametrize("hq,hkv,lengths,page_rows,q_len,layers", [
+    (28, 4, [130, 24, 10, 0], 32, 24, 1), (6, 2, [333, 50, 200, 65], 32, 20, 1), (4, 1, [300, 17, 64, 63, 65, 128, 1, 0], 16, 15, 1),
+    (57, 1, [190, 4, 64], 48, 1, 3), (16, 2, [9000, 3], 64, 100, 1)],
+    ids=lambda x: str(x) if isinstance(x, int) else "%dx%d" % (len(x), max(x)))
+def test_calls_that_the_tensor_core_kernel_takes(hq, hkv, lengths, page_rows, q_len, layers):
+    geom = cf.make_geom(hq, hkv, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, hkv, 128, lengths, page_rows, layers, seed=q_len)
+    assert cf.cf_debug_kv4_attn_kernel(geom, pages.desc, q_len, layers) == 3
+    q = torch.randn((layers, len(lengths), q_len, hq, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    assert cf.cf_pages_status(pages.desc) == 0
+    _check_attention(geom, out, lse, q, kept, 128 ** -0.5)
+    again, lse2 = _attend(geom, pages, pool, q)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("way,hq,hkv,q_len,cols,requests", [(2, 28, 4, 1, 0, 96), (0, 28, 4, 1, 3000, 96), (0, 4, 4, 1, 0, 200), (0, 12, 1, 3, 0, 300), (1, 28, 4, 1, 3000, 3), (1, 4, 4, 1, 3000, 3),
+                                                            (1, 12, 1, 3, 3000, 3), (2, 28, 4, 1, 0, 3), (2, 4, 4, 1, 0, 3), (2, 12, 1, 3, 0, 3), (3, 28, 4, 24, 0, 3)])
+def test_every_way_of_doing_a_call(way, hq, hkv, q_len, cols, requests):
+    """Shares of warps and of CTAs, clusters, the tensor cores: each is what the call takes."""
+    geom = cf.make_geom(hq, hkv, 128, torch.bfloat16, 32768, 1e6)
+    pages, pool, kept = _filled(geom, hkv, 128, [(37 * i + 290) % 321 for i in range(requests)], 32, 1, seed=hq + q_len, cols=cols or None)
+    assert cf.cf_debug_kv4_attn_kernel(geom, pages.desc, q_len, 1) == way
+    q = torch.randn((1, requests, q_len, hq, 128), generator=torch.Generator().manual_seed(4)).bfloat16().cuda()
+    out, lse = _attend(geom, pages, pool, q)
+    assert cf.cf_pages_status(pages.desc) == 0
+    _check_attention(geom, out, lse, q, kept, 128 ** -0.5)

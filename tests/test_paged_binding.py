@@ -129,3 +129,35 @@ def test_limits_of_waits_that_make_no_sense_are_refused(lib):
     for limit in (0, -1, 2000000001):
         assert call(limit, 1 << 40) == cf.CF_ERR_INVALID_ARG
     assert call(1000, 0) == cf.CF_ERR_WORKSPACE
+
+
+def _way(hq, hkv, dim, dtype, requests, page_rows, cols, q_len, layers=1):
+    pages = cf.cf_pages(requests, page_rows, 4 * requests * cols, cols, FAKE, FAKE, FAKE, FAKE, FAKE)
+    return cf.cf_debug_kv4_attn_kernel(cf.make_geom(hq, hkv, dim, dtype, 32768, 1e6), pages, q_len, layers)
+
+
+WARPS, CTAS, CLUSTERS, TCGEN05 = 0, 1, 2, 3
+
+
+@pytest.mark.parametrize("want,call", [
+    # the tensor cores from 57 query columns of a kv head and eight units of 128 on, bf16 and head_dim 128
+    (TCGEN05, (28, 4, 128, torch.bfloat16, 4, 64, 252, 24)), (TCGEN05, (8, 1, 128, torch.bfloat16, 8, 16, 30, 8)),
+    (TCGEN05, (57, 1, 128, torch.bfloat16, 8, 16, 3000, 1)), (CTAS, (56, 1, 128, torch.bfloat16, 8, 16, 3000, 1)),
+    (CTAS, (8, 1, 128, torch.bfloat16, 7, 16, 3000, 8)), (TCGEN05, (8, 1, 128, torch.bfloat16, 4, 16, 3000, 17)),
+    (CTAS, (28, 4, 64, torch.bfloat16, 4, 64, 252, 24)), (CTAS, (28, 4, 128, torch.float32, 4, 64, 252, 24)),
+    # clusters by the room of the table, fewer than six steps of 32 rows to a warp (nine with few columns), 8 CTAs of 4 (8) warps
+    (CLUSTERS, (12, 2, 128, torch.bfloat16, 1, 64, 95, 1)), (CTAS, (12, 2, 128, torch.bfloat16, 1, 64, 96, 1)),
+    (CLUSTERS, (2, 2, 128, torch.bfloat16, 1, 64, 287, 1)), (CTAS, (2, 2, 128, torch.bfloat16, 1, 64, 288, 1)),
+    (CTAS, (12, 2, 128, torch.bfloat16, 1, 64, 512, 1)),
+    # shares of single warps where units are many
+    (CTAS, (28, 4, 128, torch.bfloat16, 88, 32, 190, 1)), (WARPS, (28, 4, 128, torch.bfloat16, 89, 32, 190, 1)),
+    (WARPS, (4, 4, 128, torch.bfloat16, 700, 16, 5, 1)), (CTAS, (32, 32, 128, torch.bfloat16, 8, 64, 340, 1))])
+def test_how_a_call_is_done(lib, want, call):
+    """On both sides of the lines of the dispatch, for 148 multiprocessors."""
+    assert _way(*call) == want
+
+
+def test_how_a_call_is_done_is_asked_properly(lib):
+    pages, geom, ref = _pages(), cf.make_geom(4, 2, 64, cf.CF_BF16, 4096, 1e4), ctypes.byref
+    assert lib.cf_debug_kv4_attn_kernel(ref(geom), ref(pages), 0, 1, FAKE) == cf.CF_ERR_INVALID_ARG
+    assert lib.cf_debug_kv4_attn_kernel(ref(geom), ref(pages), 1, 1, None) == cf.CF_ERR_INVALID_ARG
