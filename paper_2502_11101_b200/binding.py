@@ -77,6 +77,7 @@ class cf_pages(ctypes.Structure):
     _fields_ = [("n_requests", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("table_cols", ctypes.c_int32),
                 ("table", ctypes.c_void_p), ("rows", ctypes.c_void_p), ("free_pages", ctypes.c_void_p),
                 ("free_count", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+    device = None                    # index of the device that the arrays are on, where make_pages has seen them
 
 
 class cf_stack(ctypes.Structure):
@@ -632,15 +633,23 @@ def cf_decode_append(geom: cf_geom, n_requests: int, cache_rows: int, k_final: t
 def make_pages(table: torch.Tensor, rows: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor, status: torch.Tensor,
                page_rows: int) -> cf_pages:
     """The pages of a batch of requests: int32 device tensors the caller keeps alive, `table` [B, columns], `rows` [B],
-    `free_pages` [pages of the pool], `free_count` [1], `status` [1].  cf_pages_init sets them up."""
+    `free_pages` [pages of the pool], `free_count` [1], `status` [1].  cf_pages_init sets them up.  Calls on them are made with their
+    device as the current one."""
     for t in (table, rows, free_pages, free_count, status):
         assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.device == table.device
     assert table.dim() == 2 and rows.shape == (table.shape[0],) and free_count.numel() == 1 and status.numel() == 1
-    return cf_pages(table.shape[0], page_rows, free_pages.numel(), table.shape[1], table.data_ptr(), rows.data_ptr(),
-                    free_pages.data_ptr(), free_count.data_ptr(), status.data_ptr())
+    pages = cf_pages(table.shape[0], page_rows, free_pages.numel(), table.shape[1], table.data_ptr(), rows.data_ptr(),
+                     free_pages.data_ptr(), free_count.data_ptr(), status.data_ptr())
+    pages.device = table.device.index
+    return pages
+
+
+def _pages_here(pages: cf_pages) -> None:
+    assert pages.device is None or pages.device == torch.cuda.current_device(), "pages on the current device are expected"
 
 
 def cf_pages_init(pages: cf_pages, stream=None) -> None:
+    _pages_here(pages)
     _check(load_library().cf_pages_init(ctypes.byref(pages), _stream(stream)), "cf_pages_init")
 
 
@@ -651,6 +660,7 @@ def cf_pages_resize(pages: cf_pages, rows: torch.Tensor, extra_rows: int = 0, sl
 
 
 def cf_pages_status(pages: cf_pages, stream=None) -> int:
+    _pages_here(pages)
     return int(load_library().cf_pages_status(ctypes.byref(pages), _stream(stream)))
 
 
@@ -694,6 +704,7 @@ def cf_debug_kv4_attn_kernel(geom: cf_geom, pages: cf_pages, q_len: int, n_layer
 def cf_debug_kv4_attn(geom: cf_geom, pages: cf_pages, kv4: torch.Tensor, q: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor,
                       limit_cycles: int, copies: bool = True, lse: Optional[torch.Tensor] = None, stream=None) -> None:
     """cf_kv4_attn on dense tensors whose waits run out after `limit_cycles`, for certain without its copies."""
+    _pages_here(pages)
     assert q.is_contiguous() and out.is_contiguous() and kv4.is_contiguous()
     _check(load_library().cf_debug_kv4_attn(ctypes.byref(geom), ctypes.byref(pages), q.shape[0], q.shape[2], q.data_ptr(), q.stride(0),
                                             kv4.data_ptr(), kv4.stride(0), 0.0, out.data_ptr(), out.stride(0), _ptr(lse), workspace.data_ptr(),

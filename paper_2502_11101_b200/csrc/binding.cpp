@@ -98,6 +98,21 @@ public:
         if (b.view.len != (Py_ssize_t)sizeof(T)) fail(PyExc_TypeError, "a structure of another size is expected");
         return static_cast<const T*>(b.view.buf);
     }
+    // pages of the current device, where make_pages has seen which one they are on
+    const cf_pages* pages(Bytes& b) {
+        const cf_pages* p = structure<cf_pages>(b);
+        static PyObject* const name = PyUnicode_InternFromString("device");
+        PyObject* device = PyObject_GetAttr(a_[i_ - 1], name);
+        if (!device) {
+            PyErr_Clear();
+            return p;
+        }
+        const long long index = device == Py_None ? -1 : PyLong_AsLongLong(device);
+        Py_DECREF(device);
+        if (index == -1 && PyErr_Occurred()) throw Raised{};
+        require(index < 0 || index == c10::cuda::current_device(), "pages on the current device are expected");
+        return p;
+    }
     // a stream object, a raw handle, or None for the current stream
     void* stream() {
         PyObject* o = next();
@@ -372,7 +387,7 @@ NATIVE(pages_resize) {                             // pages, rows, extra_rows, s
     return guarded([&] {
         Args in(argv, argc);
         Bytes bp;
-        const cf_pages* p = in.structure<cf_pages>(bp);
+        const cf_pages* p = in.pages(bp);
         const at::Tensor& rows = in.tensor();
         const int32_t extra = in.i32();
         const at::Tensor* slots = in.maybe_tensor();
@@ -428,7 +443,7 @@ NATIVE(kv4_write) {                                // geom, pages, kv4, slots, k
         Args in(argv, argc);
         Bytes bg, bp;
         const cf_geom* g = in.structure<cf_geom>(bg);
-        const cf_pages* p = in.structure<cf_pages>(bp);
+        const cf_pages* p = in.pages(bp);
         const at::Tensor &kv4 = in.tensor(), &slots = in.tensor(), &k = in.tensor(), &v = in.tensor();
         void* s = in.stream();
         const RowSpan r = row_span(g, p, kv4, slots, k, v);
@@ -444,7 +459,7 @@ NATIVE(kv4_read) {                                 // geom, pages, kv4, slots, k
         Args in(argv, argc);
         Bytes bg, bp;
         const cf_geom* g = in.structure<cf_geom>(bg);
-        const cf_pages* p = in.structure<cf_pages>(bp);
+        const cf_pages* p = in.pages(bp);
         const at::Tensor &kv4 = in.tensor(), &slots = in.tensor(), &k = in.tensor(), &v = in.tensor();
         void* s = in.stream();
         const RowSpan r = row_span(g, p, kv4, slots, k, v);
@@ -460,7 +475,7 @@ NATIVE(kv4_attn) {                                 // geom, pages, kv4, q, out, 
         Args in(argv, argc);
         Bytes bg, bp;
         const cf_geom* g = in.structure<cf_geom>(bg);
-        const cf_pages* p = in.structure<cf_pages>(bp);
+        const cf_pages* p = in.pages(bp);
         const at::Tensor &kv4 = in.tensor(), &q = in.tensor(), &out = in.tensor(), &ws = in.tensor();
         const at::Tensor* lse = in.maybe_tensor();
         const float scale = in.real();

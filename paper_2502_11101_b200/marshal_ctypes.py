@@ -113,8 +113,9 @@ def run_stack(geom, batch, plan, workspace, q, k, v, out, score_accum, schedule,
     return code, 0
 
 
-def _require_here(*tensors):
+def _require_here(pages, *tensors):
     """The calls below check what they are given: on the current device, whose stream they take."""
+    B._pages_here(pages)
     for t in tensors:
         _require(t is None or (t.is_cuda and t.get_device() == torch.cuda.current_device()), "a tensor on the current device is expected")
 
@@ -137,7 +138,7 @@ def pages_resize(pages, rows, extra_rows, slots, stream):
     _require(rows.dtype == torch.int32 and rows.is_contiguous() and rows.numel() == pages.n_requests > 0, "rows: int32, one per request")
     _require(slots is None or (slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() % pages.n_requests == 0),
              "slots: int64, as many for each request")
-    _require_here(rows, slots)
+    _require_here(pages, rows, slots)
     return B.load_library().cf_pages_resize(_ref(pages), rows.data_ptr(), extra_rows, 0 if slots is None else slots.numel() // pages.n_requests,
                                             B._ptr(slots), B._stream(stream))
 
@@ -168,7 +169,7 @@ def _rows(geom, pages, kv4, slots, k, v):
     _require(k.shape == v.shape and rows == _rows_of(geom, v), "k and v: one shape and stride")
     _require(slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == rows[1], "slots: int64, one per row of a layer")
     _require_pool(geom, pages, kv4, k.shape[0])
-    _require_here(kv4, slots, k, v)
+    _require_here(pages, kv4, slots, k, v)
     return rows
 
 
@@ -190,6 +191,6 @@ def kv4_attn(geom, pages, kv4, q, out, workspace, lse, scale, stream):
     _require(q.shape[1] == pages.n_requests and q.shape[3] == geom.n_q_heads and q.shape[4] == geom.head_dim, "q: of other sizes than the geometry and the pages")
     _require(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == q.numel() // geom.head_dim), "lse: fp32, one per query and head")
     _require_pool(geom, pages, kv4, q.shape[0])
-    _require_here(kv4, q, out, workspace, lse)
+    _require_here(pages, kv4, q, out, workspace, lse)
     return B.load_library().cf_kv4_attn(_ref(geom), _ref(pages), q.shape[0], q.shape[2], q.data_ptr(), _layer_stride(q), kv4.data_ptr(), _layer_stride(kv4),
                                         scale, out.data_ptr(), _layer_stride(out), B._ptr(lse), workspace.data_ptr(), _bytes(workspace), B._stream(stream))

@@ -214,3 +214,20 @@ def test_every_way_of_doing_a_call(way, hq, hkv, q_len, cols, requests):
     out, lse = _attend(geom, pages, pool, q)
     assert cf.cf_pages_status(pages.desc) == 0
     _check_attention(geom, out, lse, q, kept, 128 ** -0.5)
+
+
+def test_pages_of_another_device_are_refused(marshal):
+    geom, pages = cf.make_geom(1, 1, 64, torch.bfloat16, 4096, 1e4), Pages(3, 16, 10, 4)
+    assert pages.desc.device == torch.cuda.current_device()
+    slots, pool = torch.full((3, 1), -1, dtype=torch.int64, device="cuda"), torch.zeros((1, cf.cf_kv4_layer_bytes(geom, pages.desc)), dtype=torch.uint8, device="cuda")
+    k, q = torch.zeros((1, 3, 1, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros((1, 3, 1, 1, 64), dtype=torch.bfloat16, device="cuda")
+    work = torch.zeros(cf.cf_kv4_attn_workspace_bytes(geom, pages.desc, 1, 1), dtype=torch.uint8, device="cuda")
+    calls = (lambda: cf.cf_pages_init(pages.desc), lambda: cf.cf_pages_status(pages.desc), lambda: cf.cf_pages_resize(pages.desc, pages.rows, 0, slots),
+             lambda: cf.cf_kv4_write(geom, pages.desc, pool, slots, k, k), lambda: cf.cf_kv4_read(geom, pages.desc, pool, slots, k, k),
+             lambda: cf.cf_kv4_attn(geom, pages.desc, pool, q, q.clone(), work))
+    for call in calls:
+        call()
+    pages.desc.device = pages.desc.device + 1          # as if they had been made on the next one
+    for call in calls:
+        with pytest.raises(AssertionError, match="pages on the current device"):
+            call()

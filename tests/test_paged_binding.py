@@ -161,3 +161,17 @@ def test_how_a_call_is_done_is_asked_properly(lib):
     pages, geom, ref = _pages(), cf.make_geom(4, 2, 64, cf.CF_BF16, 4096, 1e4), ctypes.byref
     assert lib.cf_debug_kv4_attn_kernel(ref(geom), ref(pages), 0, 1, FAKE) == cf.CF_ERR_INVALID_ARG
     assert lib.cf_debug_kv4_attn_kernel(ref(geom), ref(pages), 1, 1, None) == cf.CF_ERR_INVALID_ARG
+
+
+def test_pages_of_another_device_are_refused(lib, monkeypatch):
+    """Their arrays would be read and written from a device that they are not on."""
+    geom, pages = cf.make_geom(1, 1, 64, torch.bfloat16, 4096, 1e4), _pages()
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    pages.device = 1
+    rows, slots, pool = torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int64), torch.zeros((1, cf.cf_kv4_layer_bytes(geom, pages)), dtype=torch.uint8)
+    k, q, work = torch.zeros((1, 3, 1, 64), dtype=torch.bfloat16), torch.zeros((1, 3, 1, 1, 64), dtype=torch.bfloat16), torch.zeros(1 << 20, dtype=torch.uint8)
+    for call in (lambda: cf.cf_pages_init(pages), lambda: cf.cf_pages_status(pages), lambda: M.pages_resize(pages, rows, 0, slots, None),
+                 lambda: M.kv4_write(geom, pages, pool, slots, k, k, None), lambda: M.kv4_read(geom, pages, pool, slots, k, k, None),
+                 lambda: M.kv4_attn(geom, pages, pool, q, q, work, None, 0.0, None), lambda: cf.cf_debug_kv4_attn(geom, pages, pool, q, q, work, 1000)):
+        with pytest.raises(AssertionError, match="pages on the current device"):
+            call()
