@@ -251,7 +251,7 @@ rows_kernel(RowArgs args, Divisor page_rows, Divisor runs, Divisor quads, int ru
 
 template <typename T, int D, bool WRITE>
 int launch_rows(const RowArgs& a, const void* k, const void* v, const void* kv4, cudaStream_t stream) {
-    const int quads = (a.n_rows + kRowsPerWarp - 1) / kRowsPerWarp;
+    const int quads = a.n_rows / kRowsPerWarp + (a.n_rows % kRowsPerWarp != 0);
     const long long warps = (long long)quads * a.n_kv_heads * a.n_layers;
     // a warp finds its rows once for several heads, where that leaves every SM the warps it holds four times over (2.4 M rows of a
     // head: writing with runs of 1, 2, 4, 8, 16 heads 415, 341, 302, 293, 301 us; reading 321, 286, 269, 274, 276)

@@ -175,3 +175,12 @@ def test_pages_of_another_device_are_refused(lib, monkeypatch):
                  lambda: M.kv4_attn(geom, pages, pool, q, q, work, None, 0.0, None), lambda: cf.cf_debug_kv4_attn(geom, pages, pool, q, q, work, 1000)):
         with pytest.raises(AssertionError, match="pages on the current device"):
             call()
+
+
+@pytest.mark.parametrize("n_rows", [(1 << 31) - 1, (1 << 31) - 3])
+def test_rows_that_are_too_many_are_refused(lib, n_rows):
+    """Their number is rounded up to fours, beyond 32 bits."""
+    geom, pages, ref = cf.make_geom(8, 8, 64, cf.CF_BF16, 4096, 1e4), _pages(), ctypes.byref
+    layer, stride = cf.cf_kv4_layer_bytes(geom, pages), n_rows * 512
+    assert lib.cf_kv4_write(ref(geom), ref(pages), 4, n_rows, FAKE, FAKE, FAKE, stride, 512, FAKE, layer, None) == cf.CF_ERR_INVALID_ARG
+    assert lib.cf_kv4_read(ref(geom), ref(pages), 4, n_rows, FAKE, FAKE, layer, FAKE, FAKE, stride, 512, None) == cf.CF_ERR_INVALID_ARG
