@@ -447,7 +447,7 @@ typedef struct cf_pages {
     int32_t n_requests;       /* 1 .. 2^20                                                            */
     int32_t page_rows;        /* rows of a page, a multiple of 16                                     */
     int32_t n_pages;          /* pages of the pool                                                    */
-    int32_t table_cols;       /* most pages of a request                                              */
+    int32_t table_cols;       /* most pages of a request; n_requests * table_cols + n_pages < 2^31     */
     int32_t* table;           /* device [n_requests][table_cols]                                      */
     int32_t* rows;            /* device [n_requests] rows in use                                      */
     int32_t* free_pages;      /* device [n_pages] a stack: the first *free_count entries are free     */

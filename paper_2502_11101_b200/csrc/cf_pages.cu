@@ -232,8 +232,8 @@ int check_pages(const cf_pages* p) {
     if (!p || p->n_requests <= 0 || p->n_requests > (1 << 20) || p->page_rows < 16 || p->page_rows % 16 != 0 || p->n_pages <= 0 ||
         p->table_cols <= 0)
         return CF_ERR_INVALID_ARG;
-    if ((long long)p->table_cols * p->page_rows > INT_MAX - 2LL * p->page_rows - 256 || (long long)p->n_requests * p->table_cols > INT_MAX)
-        return CF_ERR_INVALID_ARG;
+    if ((long long)p->table_cols * p->page_rows > INT_MAX - 2LL * p->page_rows - 256 || (long long)p->n_requests * p->table_cols + p->n_pages > INT_MAX)
+        return CF_ERR_INVALID_ARG;                // the stack's height, while pages come back, is counted in 32 bits
     if (!p->table || !p->rows || !p->free_pages || !p->free_count || !p->status) return CF_ERR_INVALID_ARG;
     return CF_OK;
 }

@@ -184,3 +184,15 @@ def test_rows_that_are_too_many_are_refused(lib, n_rows):
     layer, stride = cf.cf_kv4_layer_bytes(geom, pages), n_rows * 512
     assert lib.cf_kv4_write(ref(geom), ref(pages), 4, n_rows, FAKE, FAKE, FAKE, stride, 512, FAKE, layer, None) == cf.CF_ERR_INVALID_ARG
     assert lib.cf_kv4_read(ref(geom), ref(pages), 4, n_rows, FAKE, FAKE, layer, FAKE, FAKE, stride, 512, None) == cf.CF_ERR_INVALID_ARG
+
+
+def test_pages_and_table_entries_fit_32_bits_together(lib):
+    """The stack's height while pages come back: what it holds and what all requests release, whatever the lengths say."""
+    geom, ref = cf.make_geom(1, 1, 64, cf.CF_BF16, 4096, 1e4), ctypes.byref
+    for n_requests, cols, n_pages, fine in ((1 << 10, 1 << 20, (1 << 30) - 1, True), (1 << 10, 1 << 20, 1 << 30, False), (1, 1, (1 << 31) - 1, False),
+                                            (1, 1, (1 << 31) - 2, True), (1 << 10, (1 << 21) - 1, 1024, False), (1 << 10, (1 << 21) - 1, 1023, True)):
+        pages = cf.cf_pages(n_requests, 16, n_pages, cols, FAKE, FAKE, FAKE, FAKE, FAKE)
+        assert (cf.cf_kv4_layer_bytes(geom, pages) != 0) == fine, (n_requests, cols, n_pages)
+        if not fine:
+            assert lib.cf_pages_resize(ref(pages), FAKE, 0, 0, None, None) == cf.CF_ERR_INVALID_ARG
+            assert lib.cf_pages_init(ref(pages), None) == cf.CF_ERR_INVALID_ARG
