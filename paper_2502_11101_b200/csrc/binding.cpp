@@ -485,6 +485,7 @@ NATIVE(kv4_attn) {                                 // geom, pages, kv4, q, out, 
         require(q.size(1) == p->n_requests && q.size(3) == g->n_q_heads && q.size(4) == g->head_dim, "q: of other sizes than the geometry and the pages");
         require(!lse || (lse->scalar_type() == at::kFloat && lse->is_contiguous() && lse->numel() == q.numel() / g->head_dim),
                 "lse: fp32, one per query and head");
+        require(ws.is_contiguous(), "workspace: dense");
         require_pool(g, p, kv4, q.size(0));
         for (const at::Tensor* t : {&kv4, &q, &out, &ws}) require_here(*t);
         if (lse) require_here(*lse);

@@ -190,6 +190,7 @@ def kv4_attn(geom, pages, kv4, q, out, workspace, lse, scale, stream):
     _require(_of_storage_type(geom, q) and _of_storage_type(geom, out), "q and out: the storage type of the geometry")
     _require(q.shape[1] == pages.n_requests and q.shape[3] == geom.n_q_heads and q.shape[4] == geom.head_dim, "q: of other sizes than the geometry and the pages")
     _require(lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == q.numel() // geom.head_dim), "lse: fp32, one per query and head")
+    _require(workspace.is_contiguous(), "workspace: dense")
     _require_pool(geom, pages, kv4, q.shape[0])
     _require_here(pages, kv4, q, out, workspace, lse)
     return B.load_library().cf_kv4_attn(_ref(geom), _ref(pages), q.shape[0], q.shape[2], q.data_ptr(), _layer_stride(q), kv4.data_ptr(), _layer_stride(kv4),

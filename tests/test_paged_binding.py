@@ -196,3 +196,16 @@ def test_pages_and_table_entries_fit_32_bits_together(lib):
         if not fine:
             assert lib.cf_pages_resize(ref(pages), FAKE, 0, 0, None, None) == cf.CF_ERR_INVALID_ARG
             assert lib.cf_pages_init(ref(pages), None) == cf.CF_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("module", ["native", "ctypes"])
+def test_a_workspace_has_the_bytes_that_it_counts(lib, module):
+    """A view with gaps, or of the same byte many times, has fewer behind its address."""
+    module = binding._load_native(cf_build.NATIVE_PATH) if module == "native" else M
+    geom, pages = cf.make_geom(1, 1, 64, torch.bfloat16, 4096, 1e4), _pages()
+    pool = torch.zeros((1, cf.cf_kv4_layer_bytes(geom, pages)), dtype=torch.uint8)
+    q = torch.zeros((1, 3, 1, 1, 64), dtype=torch.bfloat16)
+    need = cf.cf_kv4_attn_workspace_bytes(geom, pages, 1, 1)
+    for work in (torch.zeros(1, dtype=torch.uint8).expand(need), torch.zeros((need // 64, 128), dtype=torch.uint8)[:, :64]):
+        with pytest.raises(AssertionError, match="workspace"):
+            module.kv4_attn(geom, pages, pool, q, q, work, None, 0.0, 0)
