@@ -480,7 +480,7 @@ size_t cf_kv4_layer_bytes(const cf_geom* geom, const cf_pages* pages);
  *   slots   device [n_rows]: where row i goes; negative: nowhere.  A slot that appears twice is left with one row's numbers or
  *           another's, which may differ from group to group
  *   k, v    device, storage type of geom: layer l's row i at l * kv_layer_stride + i * row_stride elements,
- *           [n_kv_heads][head_dim] each; strides are multiples of 16 bytes
+ *           [n_kv_heads][head_dim] each; strides are multiples of 16 bytes, and layers lie one behind the other
  *   kv4     the pool, layers kv4_layer_stride bytes apart (a multiple of 16)
  * A slot beyond the pool raises CF_ERR_RANGE in the status word and is skipped.  Nothing but the rows' slots is written.
  * n_rows / 4 * n_kv_heads * n_layers stays below 2^31. */
@@ -508,10 +508,16 @@ size_t cf_kv4_attn_workspace_bytes(const cf_geom* geom, const cf_pages* pages, i
  *   workspace  at least cf_kv4_attn_workspace_bytes(..., q_len, n_layers) bytes, 256-byte aligned; calls that share one must
  *           not overlap on the device
  * Keys and values enter the products exactly, queries of bf16 storage too (what lies below 2^-17 of a query's largest
- * component loses last bits, 2^-25 of it); probabilities are rounded to 11 bits (fp32 storage: queries and probabilities to
- * 22), sums are fp32.  (bf16, head_dim 128, more than 56 query heads x tokens per kv head: keys and values whose scales differ
- * by more than 2^28 from the largest among 16 rows lose what lies 2^-38 below that row's.)  The table may name a page several
- * times, for several requests or in one (zeros for a warm-up, a passage that is shared).  A table entry beyond the pool, or more rows than the table has room for, raises CF_ERR_RANGE in the status word; such a request's results mean nothing. */
+ * component loses last bits, 2^-25 of it); probabilities, times the values' scales, are rounded to 11 bits (fp32 storage:
+ * queries and probabilities to 22), sums are fp32.  These bits are kept down to a limit that the largest value of the request
+ * and kv head sets: each key adds at most 2^-31 of that value to the error of a result, in every dim.  So dims or rows whose
+ * values are all far below the largest keep fewer bits: below 2^-20 of it, fewer than 11.  (bf16, head_dim 128, more than 56
+ * query heads x tokens per kv head: keys and values whose scales differ by more than 2^28 from the largest among 16 rows lose
+ * what lies 2^-38 below that row's.  Where all scales are below 2^-98, a number may be off by 2^-135.)
+ * The table may name a page several times, for several requests or in one (zeros for a warm-up, a passage that is shared);
+ * cf_pages_resize makes no such table, and would give the page back once for every place.  Nothing may change the pages while
+ * a call on them runs.  A table entry beyond the pool, or more rows than the table has room for, raises CF_ERR_RANGE in the
+ * status word; such a request's results mean nothing. */
 int cf_kv4_attn(const cf_geom* geom, const cf_pages* pages, int32_t n_layers, int32_t q_len, const void* q,
                 int64_t q_layer_stride, const void* kv4, int64_t kv4_layer_stride, float softmax_scale, void* out,
                 int64_t out_layer_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream);

@@ -24,10 +24,11 @@
 //
 // Short caches do without the line: a unit has a cluster of CTAs, joined over distributed shared memory (see cut_of).
 //
-// Measured (B200, a call with its merge, caches in HBM): 8 requests of 19-21.6 K rows, 32/32 heads, 122 us until the part
-// throttles (6.1 TB/s, 0.94 of the copy rate; 134 in a loop); 96 of 17-6001 rows, 28/4, 44.5 us (3.7 TB/s); four layers of three ragged
-// requests, 32/8, 16.2 us; one of 1011 rows, 12/2, 6.2 us.  The loop issues 222 (few columns) and 282 instructions for 16 keys, 64 of
-// them conversions, at 0.57 and 0.52 per cycle and scheduler: that is what bounds grouped heads; few columns meet HBM.
+// Measured (B200, a call with its merge, caches in HBM): 8 requests of 19-21.6 K rows, 32/32 heads, 137 us call after call (5.5 TB/s,
+// 0.84 of the copy rate; 122 to 127 in a cool part); 96 of 17-6001 rows, 28/4, 44.5 us (3.7 TB/s); four layers of three ragged
+// requests, 32/8, 16.2 us; one of 1011 rows, 12/2, in a table with room for 1152, 6.2 us.  The loop issues 222 (few columns) and 282
+// instructions for 16 keys, 64 of them conversions, at 0.57 and 0.52 per cycle and scheduler.  Few columns meet HBM; grouped heads have
+// three warps to a scheduler, whose instructions and the latencies that they do not hide for one another bound them by halves.
 // What the steps of its making gave (8 long 32/32 / 96 of 28/4, us): 16 keys a step, selects under masks 171 / 69; those behind a
 // branch 162 / 68; 32 keys, shares weighed by units 148 / 51; a column per (query, group) 122 / -; four warps a CTA with 168
 // registers - / 47; shares of single warps - / 45.

@@ -1,5 +1,5 @@
-// Attention of many query columns over the 4-bit pages by the tensor cores (cf_kv4_attn from 56 query columns of a kv head on,
-// query heads times tokens; bf16 storage, head_dim 128): a follow-up question over cached documents, or the
+// Attention of many query columns over the 4-bit pages by the tensor cores (cf_kv4_attn with more than 56 query columns of a kv head,
+// query heads times tokens, and eight units; bf16 storage, head_dim 128): a follow-up question over cached documents, or the
 // verification of drafted tokens.
 //
 // A unit is 128 query columns of a (layer, request, kv head) and the request's rows, 64 at a time.  Roles of a CTA:
@@ -12,8 +12,8 @@
 // S = Q K^T with the queries as the A operand in tensor memory, O += P V with P as the A operand, there too; four S buffers and two
 // of P, so that QK^T runs two tiles ahead and neither group waits for it.  A group reads its tile's S twice, for the maximum and
 // for the probabilities; what probabilities are taken from (`base`) goes from tile to tile, so a group has to wait for the other's
-// maximum, not for its probabilities.  (One group with two S buffers 52 us, two threads to a column 51, two CTAs of one group per SM 58; this one: see
-// launch_kv4_attn_tc.)
+// maximum, not for its probabilities.  (One group with two S buffers 52 us, two threads to a column 51, two CTAs of one group per SM
+// 58, where two groups took 49; this one: see launch_kv4_attn_tc.)
 // Numbers: a code times its scale is ten bits, exact in fp16 as long as the scales of a block of 16 rows lie within 2^28 of each
 // other: a block is kept in units of 2^c, c chosen so that its largest scale comes to lie in [2^12, 2^13) (smaller ones lose last
 // bits, 2^-38 of the block's largest number and less).  Keys' units go into the logits' factor, which is the same for the 16
@@ -619,7 +619,7 @@ kv4_attn_tc_kernel(const __grid_constant__ Kv4Args args, const __grid_constant__
 
 }  // namespace
 
-// From 56 query columns on, and eight units: below, the kernel of cf_kv4_attn.cu is faster, whose units are 16 columns.  Measured
+// More than 56 query columns, and eight units: below, the kernel of cf_kv4_attn.cu is faster, whose units are 16 columns.  Measured
 // (that one / this one, us, 48, 64 and 128 columns): 4 requests of 4-16 K rows, 32/4 heads 30.1 / 30.9, 35.4 / 31.4, 59.2 / 33.8; 32 of
 // 200-2000 rows 29.8 / 35.3, 35.9 / 36.2, 61.6 / 40.0; one of 8000 rows (four units) 15.4 / 20.1, 16.4 / 20.8, 21.3 / 23.1; one of 500
 // 11.4 / 16.6, 12.1 / 16.9, 12.6 / 18.6.
@@ -628,11 +628,11 @@ bool kv4_attn_tc_supported(const cf_geom* g, int columns, double units) {
 }
 
 // 24 query tokens over 4 requests of 4-16 K rows, 28/4 heads (168 columns): 45.1 us with the join of the parts, 77 by the kernel of
-// cf_kv4_attn.cu; 13.7 GFLOP, 0.18 of the measured peak.  A tile of 64 keys takes 1700 cycles, of which its products are 512: a
-// softmax group is busy for 3400 of every two tiles, the warps of the values for 1650 of each, the MMA warp for 1600, all with
-// latencies (a wait for a barrier that is complete takes 200) at 0.45 of the issue slots.  So no role alone is what bounds it:
-// without the exponentials, the conversions, the maximum or half of the products it takes 45.8; three groups 48.9, eight warps of
-// values 48.5, both 49.6, five or eight tiles of raw blocks 47.0 and 47.8.
+// cf_kv4_attn.cu; 13.7 GFLOP, 0.19 of the measured peak.  A tile of 64 keys takes 1650 cycles, of which its products are 512, at 0.53
+// of the issue slots.  Where a tile took 1700 (46.6 us, with another loop that waits) a softmax group was busy for 3400 of every two
+// tiles, the warps of the values for 1650 of each, the MMA warp for 1600, all with latencies (a wait for a barrier that is complete
+// took 200).  So no role alone is what bounds it: from there, without the exponentials, the conversions, the maximum or half of the
+// products 45.8; three groups 48.9, eight warps of values 48.5, both 49.6, five or eight tiles of raw blocks 47.0 and 47.8.
 int launch_kv4_attn_tc(const Kv4Args& a, const PagesView& pv, cudaStream_t stream) {
     static PerDeviceOnce once;
     const int rc = configure_smem_once(once, kv4_attn_tc_kernel, kTcSmem);
